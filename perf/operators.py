@@ -112,13 +112,13 @@ def _randn(g, *shape):
 
 
 def _grouped(ids, count):
-    """Rows of ids (flat) in 0 .. count - 1, in the order of the id and then of the row; where each id's rows begin."""
+    """Rows of ids (flat) in the order of the id and then of the row, those with an id of -1 last; where each id's begin."""
     ids = ids.reshape(-1).long()
     key = torch.where(ids < 0, count, ids)
     order = torch.sort(key, stable=True)[1]
     sizes = torch.bincount(key, minlength=count + 1)[:count]
     offsets = torch.cat([sizes.new_zeros(1), sizes.cumsum(0)])
-    return torch.where(torch.arange(ids.numel(), device=ids.device) < offsets[-1], order, -1).int(), offsets.int()
+    return order.int(), offsets.int()
 
 
 def _pack(codes, scales, group):
@@ -342,8 +342,7 @@ def _route_exact(s, c):
         experts[m, :len(present)], weights[m, :len(present)] = present, w * c["scale"]
     flat = experts.reshape(-1)
     by_expert = [np.flatnonzero(flat == e) for e in range(E)]
-    order = np.concatenate(by_expert)
-    order = np.concatenate([order, np.full(flat.size - order.size, -1)]).astype(np.int32)
+    order = np.concatenate(by_expert + [np.flatnonzero(flat < 0)]).astype(np.int32)
     offsets = np.cumsum([0] + [v.size for v in by_expert]).astype(np.int32)
     return dict(experts=experts, weights=weights, order=order, offsets=offsets)
 
