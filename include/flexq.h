@@ -370,6 +370,96 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
                                      int N, int K, uint16_t *y, int32_t *acc_out,
                                      void *stream);
 
+/*
+ * Rows that choose their own weights: experts, and the adapters of many requests.
+ *
+ * A GROUPING of `rows` rows over `count` groups (at most FLEXQ_MAX_EXPERTS) is two device arrays:
+ *   order    int32 [rows]       every row once: those of group 0, then group 1, ..., each group's in
+ *                               ascending order, and last the rows of no group
+ *   offsets  int32 [count + 1]  group g is order[offsets[g]] .. order[offsets[g + 1] - 1]; offsets[0] = 0,
+ *                               offsets[count] = the number of rows that have a group
+ * flexq_group_rows makes it from ids (dev, int32 [rows]; an id outside 0 .. count - 1 is of no group), with
+ * the same result every time.  Workspace: flexq_group_rows_workspace_bytes(rows, count) bytes, 16-byte
+ * aligned, its content does not matter; calls that share it must be ordered on one stream.  A program keeps
+ * a grouping as long as it holds: that of a batch's adapters, for all layers of a step.
+ *
+ * flexq_route: routing to experts.  Scores of token m, from logits l (dev, [M,E], fp32 or, with half = 1,
+ * fp16, 16-byte aligned):
+ *   s = softmax(l) over the token's experts (FLEXQ_SCORE_SOFTMAX) or 1 / (1 + exp(-l)) (FLEXQ_SCORE_SIGMOID),
+ *   c = s + bias[e] (dev, fp32 [E], finite; NULL: c = s).
+ * The E experts are `groups` groups of E / groups that follow each other; with top_groups < groups only the
+ * top_groups best groups are kept, a group being worth the sum of its group_top (1 or 2) best c.  Of what is
+ * kept the k best c are chosen, ties go to the lowest index; their weights are s * scale, or with
+ * renormalise s / (sum of the k chosen s) * scale.  An expert whose logit is -inf or NaN is not there: it
+ * has no part in the softmax and is never chosen, and counts nothing in its group; +inf counts as the
+ * largest finite fp32.  Where fewer than k are there (a padding token: a row of -inf) the remaining slots are
+ * expert -1 with weight 0.
+ *   experts  dev, out, int32 [M,k], by falling c        weights  dev, out, fp32 [M,k]
+ *   order, offsets  dev, out, or both NULL: the grouping of the M k slots (slot m k + j) over the E experts
+ *   workspace       as for flexq_group_rows, flexq_route_workspace_bytes(M, E, k); may be NULL without order
+ * c is made and compared in 64 bits where a bias or a sum enters it, and the logits themselves are
+ * compared where none does; weights are good to a few ulp of fp32.
+ * 1 <= k <= FLEXQ_MAX_EXPERTS_PER_TOKEN, k <= top_groups * E / groups, groups <= 64, 0 < scale < inf.
+ *
+ * flexq_expert_linear: the linear layer (flexq_gemm_w6a6 / _w6a8, codes of either width) of E experts on
+ * rows grouped by expert.
+ *   packed   dev, E packed buffers one after the other, each flexq_packed_bytes(N, K, group) long
+ *   order, offsets   the grouping of `slots` slots over the E experts
+ *   xq, sx   dev, codes int8 [x_rows,K] and scales fp16 [x_rows].  k > 0: rows of tokens (x_rows k = slots),
+ *            slot s takes row s / k; k = 0: rows that are sorted already (x_rows = slots), as this call leaves them
+ *   y        dev, out, fp16 [slots,N]: row r is that of slot order[r] (sorted rows), or with scatter = 1 row s
+ *            is slot s.  Rows of slots without an expert are left as they were.  Must not overlap the inputs.
+ * Same values as the dense call with that expert's weights, shapes and status codes as there; x_rows K and
+ * 0.75 N K must be below 2^32.
+ * A feed-forward layer: flexq_route; flexq_quant_act or flexq_rmsnorm_quant of the tokens; gate|up with k and
+ * scatter 0; flexq_swiglu_quant of all sorted rows (rows behind the last have any content); down with k = 0
+ * and scatter = 1; flexq_expert_combine.
+ *
+ * flexq_expert_combine: out[m] = fp16( add[m] + sum_j weights[m][j] * y[m k + j] ), in fp32, j ascending, over
+ * the slots whose expert is not negative; y fp16 [M k,N], add fp16 [M,N] or NULL (a shared expert's output, the
+ * residual; may be out), out fp16 [M,N]; N a multiple of 32.
+ *
+ * flexq_adapters: low-rank adapters beside a projection y that all rows of a batch share,
+ *   out[m] = fp16( y[m] + scale[l] * B_l (A_l x[m]) ),   l the adapter of row m; out[m] = y[m] without one.
+ *   a, b     dev, fp16 [L,R,K] and [L,N,R], 16-byte aligned: the L adapters, R (a multiple of 16, at most
+ *            FLEXQ_MAX_RANK) the largest rank, shorter ones padded with zero rows of A (and finite values of B)
+ *   scale    dev, fp32 [L], finite
+ *   x, y     dev, fp16 [M,K] (the projection's input) and [M,N];  out  dev, fp16 [M,N], may be y
+ *   order, offsets   the grouping of the M rows over the L adapters
+ *   workspace   flexq_adapters_workspace_bytes(M, L, R, K) bytes, 16-byte aligned, any content
+ * fp32 sums in a fixed order, the intermediate A x to 2^-22 of itself (2^-38 of the row's largest), one rounding.
+ * K % 128 == 0, K <= FLEXQ_MAX_K, N % 32 == 0, M <= 2^24.
+ */
+#define FLEXQ_MAX_EXPERTS 512
+#define FLEXQ_MAX_EXPERTS_PER_TOKEN 16
+#define FLEXQ_MAX_RANK 256
+enum { FLEXQ_SCORE_SOFTMAX = 0, FLEXQ_SCORE_SIGMOID = 1 };
+
+typedef struct {
+    int k, score;
+    int groups, top_groups, group_top;
+    int renormalise;
+    float scale;
+    const float *bias;
+} flexq_routing;
+
+size_t flexq_group_rows_workspace_bytes(int rows, int count);
+flexq_status flexq_group_rows(const int32_t *ids, int rows, int count, int32_t *order, int32_t *offsets,
+                              void *workspace, size_t workspace_bytes, void *stream);
+size_t flexq_route_workspace_bytes(int M, int E, int k);
+flexq_status flexq_route(const void *logits, int half, int M, int E, const flexq_routing *R, int32_t *experts,
+                         float *weights, int32_t *order, int32_t *offsets, void *workspace, size_t workspace_bytes,
+                         void *stream);
+flexq_status flexq_expert_linear(const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx,
+                                 int x_rows, const int32_t *order, const int32_t *offsets, int slots, int k,
+                                 int scatter, int N, int K, uint16_t *y, void *stream);
+flexq_status flexq_expert_combine(const uint16_t *y, const int32_t *experts, const float *weights,
+                                  const uint16_t *add, int M, int k, int N, uint16_t *out, void *stream);
+size_t flexq_adapters_workspace_bytes(int M, int L, int R, int K);
+flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *scale, int L, int R, const uint16_t *x,
+                            const int32_t *order, const int32_t *offsets, int M, int N, int K, const uint16_t *y,
+                            uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

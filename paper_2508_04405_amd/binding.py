@@ -5,6 +5,7 @@ device pointers and the current HIP stream through the C ABI declared in
 include/flexq.h, and returns torch tensors.  There is no CPU fallback: if the
 library is missing or a call fails, an exception is raised.
 """
+import collections
 import ctypes
 import os
 
@@ -25,6 +26,12 @@ class _Layer(ctypes.Structure):
                 ("w_down", ctypes.c_void_p), ("gamma_attn", ctypes.c_void_p), ("gamma_ffn", ctypes.c_void_p),
                 ("eps", ctypes.c_float), ("bits_qkv", ctypes.c_int), ("bits_o", ctypes.c_int),
                 ("bits_gate_up", ctypes.c_int), ("bits_down", ctypes.c_int)]
+
+
+class _Routing(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int), ("score", ctypes.c_int), ("groups", ctypes.c_int), ("top_groups", ctypes.c_int),
+                ("group_top", ctypes.c_int), ("renormalise", ctypes.c_int), ("scale", ctypes.c_float),
+                ("bias", ctypes.c_void_p)]
 
 
 class _LayerIO(ctypes.Structure):
@@ -88,6 +95,22 @@ def load():
                                         vp, c_size, vp]
     lib.flexq_gemv_w6a8_noalloc.restype = c_int
     lib.flexq_gemv_w6a8_noalloc.argtypes = [vp, c_int, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp]
+    lib.flexq_group_rows_workspace_bytes.restype = c_size
+    lib.flexq_group_rows_workspace_bytes.argtypes = [c_int, c_int]
+    lib.flexq_group_rows.restype = c_int
+    lib.flexq_group_rows.argtypes = [vp, c_int, c_int, vp, vp, vp, c_size, vp]
+    lib.flexq_route_workspace_bytes.restype = c_size
+    lib.flexq_route_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    lib.flexq_route.restype = c_int
+    lib.flexq_route.argtypes = [vp, c_int, c_int, c_int, ctypes.POINTER(_Routing), vp, vp, vp, vp, vp, c_size, vp]
+    lib.flexq_expert_linear.restype = c_int
+    lib.flexq_expert_linear.argtypes = [vp, c_int, c_int, vp, vp, c_int, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, vp]
+    lib.flexq_expert_combine.restype = c_int
+    lib.flexq_expert_combine.argtypes = [vp, vp, vp, vp, c_int, c_int, c_int, vp, vp]
+    lib.flexq_adapters_workspace_bytes.restype = c_size
+    lib.flexq_adapters_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
+    lib.flexq_adapters.restype = c_int
+    lib.flexq_adapters.argtypes = [vp, vp, vp, c_int, c_int, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, c_size, vp]
     _lib = lib
     return lib
 
@@ -405,3 +428,128 @@ def layer_linears(layer, M, workspace, first_stage=0, last_stage=3, **buffers):
     io = layer_io(layer, M, buffers)
     _check(load().flexq_layer_linears(ctypes.byref(layer.c), M, ctypes.byref(io), first_stage, last_stage,
                                       _ptr(workspace), workspace.numel(), _stream()))
+
+
+# ---- rows that choose their own weights: experts, adapters -------------------------------------
+
+Routing = collections.namedtuple("Routing", "experts weights order offsets")
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _here(t, dtype, *shape):
+    """A contiguous tensor of this type and shape on the current device (whose stream the call uses)."""
+    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
+        raise FlexQError(f"flexq: a tensor is on {t.device}, the call runs on the current device")
+    if t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise FlexQError(f"flexq: expected a contiguous {dtype} tensor of {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return t
+
+
+def _scratch(nbytes, given, device):
+    if nbytes == 0:
+        raise FlexQError("flexq: invalid shape for workspace")
+    return given if given is not None else torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def group_rows(ids, count, workspace=None):
+    """int32 ids (any shape; outside 0 .. count - 1: no group) -> (order, offsets): the rows by group, each
+    group's in ascending order, those without one last, and where each group begins."""
+    lib = load()
+    _here(ids, torch.int32, *ids.shape)
+    rows = ids.numel()
+    ws = _scratch(lib.flexq_group_rows_workspace_bytes(rows, count), workspace, ids.device)
+    order = torch.empty(rows, dtype=torch.int32, device=ids.device)
+    offsets = torch.empty(count + 1, dtype=torch.int32, device=ids.device)
+    _check(lib.flexq_group_rows(_ptr(ids), rows, count, _ptr(order), _ptr(offsets), _ptr(ws), ws.numel(), _stream()))
+    return order, offsets
+
+
+def route_experts(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_top=1, renormalise=True,
+                  scale=1.0, group=True, workspace=None):
+    """Scores of the experts, fp32 or fp16 [M,E] -> Routing(experts int32 [M,k], weights fp32 [M,k], and with
+    `group` the grouping (order, offsets) of the M * k slots by expert, else None)."""
+    lib = load()
+    if score not in _SCORES:
+        raise FlexQError(f"flexq: score is one of {sorted(_SCORES)}, got {score!r}")
+    if logits.dtype not in (torch.float32, torch.float16) or logits.dim() != 2:
+        raise FlexQError(f"flexq: logits are fp32 or fp16 [M, E], got {logits.dtype} {list(logits.shape)}")
+    M, E = logits.shape
+    _here(logits, logits.dtype, M, E)
+    if bias is not None:
+        _here(bias, torch.float32, E)
+    dev = logits.device
+    r = _Routing(k, _SCORES[score], groups, top_groups, group_top, int(bool(renormalise)), float(scale), _ptr(bias))
+    ws = _scratch(lib.flexq_route_workspace_bytes(M, E, k), workspace, dev) if group else None
+    experts = torch.empty((M, k), dtype=torch.int32, device=dev)
+    weights = torch.empty((M, k), dtype=torch.float32, device=dev)
+    order = torch.empty(M * k, dtype=torch.int32, device=dev) if group else None
+    offsets = torch.empty(E + 1, dtype=torch.int32, device=dev) if group else None
+    _check(lib.flexq_route(_ptr(logits), int(logits.dtype == torch.float16), M, E, ctypes.byref(r), _ptr(experts),
+                           _ptr(weights), _ptr(order), _ptr(offsets), _ptr(ws), ws.numel() if group else 0, _stream()))
+    return Routing(experts, weights, order, offsets)
+
+
+def pack_experts(wq, sw, group=0):
+    """int8 codes [E,N,K] and fp16 scales [E,N] or [E,N,K/128] -> uint8 [E, packed_bytes(N, K, group)]."""
+    E, N, K = wq.shape
+    packed = torch.empty((E, packed_bytes(N, K, group)), dtype=torch.uint8, device=wq.device)
+    for e in range(E):
+        packed[e] = pack_w6(wq[e], sw[e], group)
+    return packed
+
+
+def expert_linear(packed, N, K, xq, sx, order, offsets, group=0, k=0, scatter=False, out=None):
+    """The linear layer of E experts (packed uint8 [E, packed_bytes(N, K, group)], pack_experts) on rows grouped
+    by expert -> fp16 [slots, N]: sorted rows, or with `scatter` row s for slot s.  k > 0: xq and sx are
+    tokens' rows, k slots each; k = 0: sorted rows.  Rows of slots without an expert are left as they were."""
+    lib = load()
+    nbytes = lib.flexq_packed_bytes(N, K, group)
+    if nbytes == 0:
+        raise FlexQError("flexq: invalid shape or group of the experts' weights")
+    E, slots, rows = packed.shape[0], order.numel(), xq.shape[0]
+    _here(packed, torch.uint8, E, nbytes)
+    _here(xq, torch.int8, rows, K)
+    _here(sx, torch.float16, rows)
+    _here(order, torch.int32, slots)
+    _here(offsets, torch.int32, E + 1)
+    y = torch.empty((slots, N), dtype=torch.float16, device=xq.device) if out is None else _here(out, torch.float16, slots, N)
+    _check(lib.flexq_expert_linear(_ptr(packed), E, group, _ptr(xq), _ptr(sx), rows, _ptr(order), _ptr(offsets), slots, k,
+                                   int(bool(scatter)), N, K, _ptr(y), _stream()))
+    return y
+
+
+def combine_experts(y, experts, weights, add=None, out=None):
+    """The weighted sum over each token's slots: fp16 y [M * k, N] by slot, experts int32 and weights fp32 [M,k],
+    plus fp16 add [M,N] if given -> fp16 [M,N].  Slots with a negative expert are left out."""
+    lib = load()
+    M, k = experts.shape
+    N = y.shape[1]
+    _here(y, torch.float16, M * k, N)
+    _here(experts, torch.int32, M, k)
+    _here(weights, torch.float32, M, k)
+    if add is not None:
+        _here(add, torch.float16, M, N)
+    res = torch.empty((M, N), dtype=torch.float16, device=y.device) if out is None else _here(out, torch.float16, M, N)
+    _check(lib.flexq_expert_combine(_ptr(y), _ptr(experts), _ptr(weights), _ptr(add), M, k, N, _ptr(res), _stream()))
+    return res
+
+
+def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
+    """y + scale[l] * B_l (A_l x) for rows grouped by adapter l: a fp16 [L,R,K], b fp16 [L,N,R], scale fp32 [L],
+    x fp16 [M,K], y fp16 [M,N], (order, offsets) from group_rows(ids, L); rows without an adapter keep y.
+    `out` may be y."""
+    lib = load()
+    L, R, K = a.shape
+    M, N = y.shape
+    _here(a, torch.float16, L, R, K)
+    _here(b, torch.float16, L, N, R)
+    _here(scale, torch.float32, L)
+    _here(x, torch.float16, M, K)
+    _here(y, torch.float16, M, N)
+    _here(order, torch.int32, M)
+    _here(offsets, torch.int32, L + 1)
+    ws = _scratch(lib.flexq_adapters_workspace_bytes(M, L, R, K), workspace, x.device)
+    res = torch.empty((M, N), dtype=torch.float16, device=x.device) if out is None else _here(out, torch.float16, M, N)
+    _check(lib.flexq_adapters(_ptr(a), _ptr(b), _ptr(scale), L, R, _ptr(x), _ptr(order), _ptr(offsets), M, N, K, _ptr(y),
+                              _ptr(res), _ptr(ws), ws.numel(), _stream()))
+    return res

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflexq.so")
 DEV_LIB = os.path.join(HERE, "libflexq_dev.so")
 SOURCES = ["quant_pack.hip", "producers.hip", "skinny.hip", "gemm.hip", "gemm_wlds.hip", "decode_block.hip", "layer.hip",
-           "noalloc.hip", "api.hip"]
+           "noalloc.hip", "api.hip", "routing.hip", "experts.hip", "adapters.hip"]
 DEV_SOURCES = SOURCES + ["probes.hip", "dev_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

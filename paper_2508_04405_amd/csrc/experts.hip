@@ -1,0 +1,221 @@
+// Linear layers of experts: rows grouped by expert, each group through its own packed weights, and
+// the weighted sum over the experts of a token.
+//
+//   y[r, n] = fp16( sx[i] * sw[e][n] * sum_k xq[i][k] wq[e][n][k] ),   offsets[e] <= r < offsets[e + 1],
+//
+// i the input row of sorted row r (order[r] / k for token rows, r itself for rows that are sorted
+// already), the sum exact in int32 (group-128 scales: per group, then fp32), as in the dense layers.
+#include "../../include/flexq.h"
+#include "flexq_device.h"
+#include "flexq_kernels.h"
+#include "row_groups.h"
+
+namespace {
+
+struct ExpertArgs {
+    const uint8_t *packed;       // of expert 0; the next follows expert_bytes later
+    size_t expert_bytes;
+    const int8_t *xq;            // [x_rows, K]
+    const uint16_t *sx;          // [x_rows]
+    const int32_t *order, *offsets;
+    int E, slots, x_rows, k;     // k: slots of a token, 0 = input rows are the sorted rows
+    int scatter;                 // output row order[r] instead of r
+    int N, K;
+    uint16_t *y;                 // [slots, N]
+};
+
+// A workgroup: one expert, 32 output channels, the expert's rows 32 at a time.
+template <int GROUP, int P, int W>
+__global__ __launch_bounds__(64 * W) void expert_stream_kernel(ExpertArgs a)
+{
+    __shared__ int red[W][4][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row_blocks = a.N / 32, KT = a.K / FLEXQ_TILE_K;
+    const int nb = blockIdx.x % row_blocks;
+    const RowGroup g = find_piece(a.offsets, a.E, a.slots, 0, blockIdx.x / row_blocks);
+    if (g.id < 0) return;
+    const uint8_t *base = a.packed + (size_t)g.id * a.expert_bytes;
+    const v4i *tiles = reinterpret_cast<const v4i *>(base) + (size_t)nb * KT * (FLEXQ_TILE_BYTES / 16);
+    const uint16_t *scales = reinterpret_cast<const uint16_t *>(base + (size_t)a.N * a.K / 4 * 3);
+
+    for (int r0 = g.begin; r0 < g.end; r0 += 32) {
+        const int rows = min(32, g.end - r0);
+        const int r = r0 + (lane & 31);
+        const bool live = (lane & 31) < rows;
+        int slot = 0, in = 0;
+        if (live) {
+            slot = min(max(a.order[r], 0), a.slots - 1);
+            in = a.k ? min(slot / a.k, a.x_rows - 1) : r;
+        }
+        const int8_t *x = a.xq + (size_t)in * a.K + 16 * (lane >> 5);
+        const float sx = live ? h2f(a.sx[in]) : 0.0f;
+
+        struct Stage {
+            PackedTile w;
+            v4i x[4];
+            uint16_t gs;
+        } st[P];
+        auto load = [&](Stage &s, int t) {
+            s.w = load_packed_tile(tiles + (size_t)t * (FLEXQ_TILE_BYTES / 16), lane);
+            if (live) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s.x[j] = *reinterpret_cast<const v4i *>(x + (size_t)t * FLEXQ_TILE_K + 32 * j);
+            }
+            if (GROUP) s.gs = scales[((size_t)nb * KT + t) * 32 + (lane & 31)];
+        };
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (wave + W * p < KT) load(st[p], wave + W * p);
+        v16i acc;
+        v16f facc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            acc[i] = 0;
+            facc[i] = 0.0f;
+        }
+        for (int t = wave; t < KT;) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (t < KT) {
+                    if (GROUP) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[i] = 0;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc = mfma_i8(st[p].x[j], unpack_kstep(st[p].w, j), acc);
+                    if (GROUP) {
+                        const float gs = h2f(st[p].gs);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) facc[i] = __builtin_fmaf((float)acc[i], gs, facc[i]);
+                    }
+                    if (t + W * P < KT) load(st[p], t + W * P);
+                    t += W;
+                }
+            }
+        }
+        // the wavefronts' sums meet in LDS, eight rows at a time
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (8 * q >= rows) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][i][lane] = GROUP ? __float_as_int(facc[4 * q + i]) : acc[4 * q + i];
+            __syncthreads();
+            for (int i = wave; i < 4; i += W) {
+                const int m = mfma_row(4 * q + i, lane);
+                const int n = 32 * nb + (lane & 31);
+                float v;
+                if (GROUP) {
+                    float f = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) f += __int_as_float(red[w][i][lane]);
+                    v = f * 0.25f;
+                } else {
+                    int s = 0;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) s += red[w][i][lane];
+                    v = (float)(s >> 2);
+                }
+                const float xs = __shfl(sx, m & 31, 64);
+                const int to = __shfl(slot, m & 31, 64);
+                if (m < rows)
+                    a.y[(size_t)(a.scatter ? to : r0 + m) * a.N + n] =
+                        f2h(GROUP ? v * xs : v * (xs * h2f(scales[n])));
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// out[t] = fp16( add[t] + sum_j weights[t][j] * y[t k + j] ), the sum in fp32 in the order of j.
+__global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const int32_t *experts, const float *weights,
+                                                      const uint16_t *add, int M, int k, int N, uint16_t *out)
+{
+    const int chunks = N / 8;
+    const long at = (long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (long)M * chunks) return;
+    const long m = at / chunks;
+    const int c = (int)(at - m * chunks);
+    float sum[8];
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (add) v = reinterpret_cast<const uint4 *>(add + m * N)[c];
+    auto half = [](const uint4 &q, int i) {
+        const unsigned w = i < 2 ? q.x : i < 4 ? q.y : i < 6 ? q.z : q.w;
+        return h2f((uint16_t)(w >> (16 * (i & 1))));
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = half(v, i);
+    for (int j = 0; j < k; ++j) {
+        if (experts[m * k + j] < 0) continue;
+        const float w = weights[m * k + j];
+        v = reinterpret_cast<const uint4 *>(y + (m * k + j) * N)[c];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(w, half(v, i), sum[i]);
+    }
+    unsigned o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (unsigned)f2h(sum[2 * i]) | ((unsigned)f2h(sum[2 * i + 1]) << 16);
+    reinterpret_cast<uint4 *>(out + m * N)[c] = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+template <int GROUP>
+hipError_t launch_stream(const ExpertArgs &a, hipStream_t st)
+{
+    const unsigned groups = (unsigned)(a.E < a.slots ? a.E : a.slots);
+    hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 4>), dim3(groups * (unsigned)(a.N / 32)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+flexq_status flexq_expert_linear(const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx, int x_rows,
+                                 const int32_t *order, const int32_t *offsets, int slots, int k, int scatter, int N,
+                                 int K, uint16_t *y, void *stream)
+{
+    if (!packed || !xq || !sx || !order || !offsets || !y) return FLEXQ_EINVAL;
+    if (E < 1 || x_rows < 1 || slots < 1 || k < 0 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN || (scatter != 0 && scatter != 1))
+        return FLEXQ_EINVAL;
+    if (k ? (long)x_rows * k != slots : x_rows != slots) return FLEXQ_EINVAL;
+    const size_t bytes = flexq_packed_bytes(N, K, group);
+    if (bytes == 0) return N < 1 || K < 1 || (group != 0 && group != 128) ? FLEXQ_EINVAL : FLEXQ_ESHAPE;
+    if (E > FLEXQ_MAX_EXPERTS || (long)x_rows * K >= (1L << 32) || (long)N * K / 4 * 3 >= (1L << 32)) return FLEXQ_ESHAPE;
+    if (!aligned16(packed) || !aligned16(xq) || !aligned16(y) || !aligned4(order) || !aligned4(offsets)) return FLEXQ_EALIGN;
+    ExpertArgs a{};
+    a.packed = (const uint8_t *)packed;
+    a.expert_bytes = bytes;
+    a.xq = xq;
+    a.sx = sx;
+    a.order = order;
+    a.offsets = offsets;
+    a.E = E;
+    a.slots = slots;
+    a.x_rows = x_rows;
+    a.k = k;
+    a.scatter = scatter;
+    a.N = N;
+    a.K = K;
+    a.y = y;
+    hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = group ? launch_stream<1>(a, st) : launch_stream<0>(a, st);
+    return e == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+flexq_status flexq_expert_combine(const uint16_t *y, const int32_t *experts, const float *weights, const uint16_t *add,
+                                  int M, int k, int N, uint16_t *out, void *stream)
+{
+    if (!y || !experts || !weights || !out || M < 1 || N < 1 || k < 1 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN) return FLEXQ_EINVAL;
+    if (N % 32 != 0 || (long)M * N / 8 >= (1L << 31) * 256) return FLEXQ_ESHAPE;
+    if (!aligned16(y) || !aligned16(out) || (add && !aligned16(add)) || !aligned4(experts) || !aligned4(weights))
+        return FLEXQ_EALIGN;
+    const unsigned blocks = (unsigned)(((long)M * (N / 8) + 255) / 256);
+    hipLaunchKernelGGL(combine_kernel, dim3(blocks), dim3(256), 0, (hipStream_t)stream, y, experts, weights, add, M, k, N, out);
+    return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+}  // extern "C"
+#pragma GCC visibility pop
