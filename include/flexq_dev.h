@@ -98,6 +98,16 @@ flexq_status flexq_dev_layer_linears(const flexq_dev_tuning *tuning, const flexq
                                      int *launched);
 
 /*
+ * flexq_expert_linear with a forced kernel: form 1 = streaming, 2, 3, 4 = tiles of 64 x 128, 128 x 128,
+ * 128 x 256 (with group-128 scales 4 runs 3), 0 = the library's choice; *dispatched (may be NULL) receives
+ * the form.  Per-channel scales give the same bits in every form.
+ */
+flexq_status flexq_dev_expert_linear(int form, const void *packed, int E, int group, const int8_t *xq,
+                                     const uint16_t *sx, int x_rows, const int32_t *order, const int32_t *offsets,
+                                     int slots, int k, int scatter, int N, int K, uint16_t *y, void *stream,
+                                     int *dispatched);
+
+/*
  * Measurement helpers (no arithmetic of the method): the ceilings a roofline
  * fraction can be read against on the machine at hand.
  *

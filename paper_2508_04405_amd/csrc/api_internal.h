@@ -49,4 +49,9 @@ bool streams_as_eight(int M, int N, int K);
 flexq_status layer_impl(const Tuning &tune, const flexq_layer *L, int M, const flexq_layer_io *io, int first_stage,
                         int last_stage, void *workspace, size_t workspace_bytes, void *stream, int *launched);
 
+// flexq_expert_linear with a forced form (0 = automatic; the codes of choose_form in experts.hip).
+flexq_status expert_impl(int form, const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx, int x_rows,
+                         const int32_t *order, const int32_t *offsets, int slots, int k, int scatter, int N, int K,
+                         uint16_t *y, void *stream, int *dispatched);
+
 }  // namespace flexq

@@ -54,5 +54,14 @@ flexq_status flexq_dev_layer_linears(const flexq_dev_tuning *tuning, const flexq
     return flexq::layer_impl(t, layer, M, io, first_stage, last_stage, workspace, workspace_bytes, stream, launched);
 }
 
+flexq_status flexq_dev_expert_linear(int form, const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx,
+                                     int x_rows, const int32_t *order, const int32_t *offsets, int slots, int k,
+                                     int scatter, int N, int K, uint16_t *y, void *stream, int *dispatched)
+{
+    if (form < 0 || form > 4) return FLEXQ_EINVAL;
+    return flexq::expert_impl(form, packed, E, group, xq, sx, x_rows, order, offsets, slots, k, scatter, N, K, y, stream,
+                              dispatched);
+}
+
 }  // extern "C"
 #pragma GCC visibility pop

@@ -7,26 +7,17 @@
 // already), the sum exact in int32 (group-128 scales: per group, then fp32), as in the dense layers.
 #include "../../include/flexq.h"
 #include "flexq_device.h"
+#include "api_internal.h"
 #include "flexq_kernels.h"
 #include "row_groups.h"
 
 namespace {
 
-struct ExpertArgs {
-    const uint8_t *packed;       // of expert 0; the next follows expert_bytes later
-    size_t expert_bytes;
-    const int8_t *xq;            // [x_rows, K]
-    const uint16_t *sx;          // [x_rows]
-    const int32_t *order, *offsets;
-    int E, slots, x_rows, k;     // k: slots of a token, 0 = input rows are the sorted rows
-    int scatter;                 // output row order[r] instead of r
-    int N, K;
-    uint16_t *y;                 // [slots, N]
-};
+using flexq::ExpertLinear;
 
 // A workgroup: one expert, 32 output channels, the expert's rows 32 at a time.
 template <int GROUP, int P, int W>
-__global__ __launch_bounds__(64 * W) void expert_stream_kernel(ExpertArgs a)
+__global__ __launch_bounds__(64 * W) void expert_stream_kernel(ExpertLinear a)
 {
     __shared__ int red[W][4][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -34,7 +25,7 @@ __global__ __launch_bounds__(64 * W) void expert_stream_kernel(ExpertArgs a)
     const int nb = blockIdx.x % row_blocks;
     const RowGroup g = find_piece(a.offsets, a.E, a.slots, 0, blockIdx.x / row_blocks);
     if (g.id < 0) return;
-    const uint8_t *base = a.packed + (size_t)g.id * a.expert_bytes;
+    const uint8_t *base = static_cast<const uint8_t *>(a.packed) + (size_t)g.id * a.expert_bytes;
     const v4i *tiles = reinterpret_cast<const v4i *>(base) + (size_t)nb * KT * (FLEXQ_TILE_BYTES / 16);
     const uint16_t *scales = reinterpret_cast<const uint16_t *>(base + (size_t)a.N * a.K / 4 * 3);
 
@@ -161,22 +152,32 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 template <int GROUP>
-hipError_t launch_stream(const ExpertArgs &a, hipStream_t st)
+hipError_t launch_stream(const ExpertLinear &a, hipStream_t st)
 {
     const unsigned groups = (unsigned)(a.E < a.slots ? a.E : a.slots);
     hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 4>), dim3(groups * (unsigned)(a.N / 32)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
+// 1 streaming, 2 .. 4 tiles of 64 x 128, 128 x 128, 128 x 256.
+int choose_form(const ExpertLinear &a)
+{
+    const long groups = a.E < a.slots ? a.E : a.slots;
+    const double rows = (double)a.slots / (double)groups;
+    if (rows <= 32.0) return 1;
+    if (rows <= 64.0) return 2;
+    return a.group ? 3 : 4;
+}
+
 }  // namespace
 
-#pragma GCC visibility push(default)
-extern "C" {
+namespace flexq {
 
-flexq_status flexq_expert_linear(const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx, int x_rows,
-                                 const int32_t *order, const int32_t *offsets, int slots, int k, int scatter, int N,
-                                 int K, uint16_t *y, void *stream)
+flexq_status expert_impl(int form, const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx, int x_rows,
+                         const int32_t *order, const int32_t *offsets, int slots, int k, int scatter, int N, int K,
+                         uint16_t *y, void *stream, int *dispatched)
 {
+    if (dispatched) *dispatched = 0;
     if (!packed || !xq || !sx || !order || !offsets || !y) return FLEXQ_EINVAL;
     if (E < 1 || x_rows < 1 || slots < 1 || k < 0 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN || (scatter != 0 && scatter != 1))
         return FLEXQ_EINVAL;
@@ -185,11 +186,13 @@ flexq_status flexq_expert_linear(const void *packed, int E, int group, const int
     if (bytes == 0) return N < 1 || K < 1 || (group != 0 && group != 128) ? FLEXQ_EINVAL : FLEXQ_ESHAPE;
     if (E > FLEXQ_MAX_EXPERTS || (long)x_rows * K >= (1L << 32) || (long)N * K / 4 * 3 >= (1L << 32)) return FLEXQ_ESHAPE;
     if (!aligned16(packed) || !aligned16(xq) || !aligned16(y) || !aligned4(order) || !aligned4(offsets)) return FLEXQ_EALIGN;
-    ExpertArgs a{};
-    a.packed = (const uint8_t *)packed;
+    ExpertLinear a{};
+    a.packed = packed;
     a.expert_bytes = bytes;
     a.xq = xq;
     a.sx = sx;
+    a.group = group;
+    a.split_k = 1;
     a.order = order;
     a.offsets = offsets;
     a.E = E;
@@ -201,8 +204,26 @@ flexq_status flexq_expert_linear(const void *packed, int E, int group, const int
     a.K = K;
     a.y = y;
     hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = group ? launch_stream<1>(a, st) : launch_stream<0>(a, st);
+    if (form == 0) form = choose_form(a);
+    if (dispatched) *dispatched = form;
+    hipError_t e;
+    if (form == 1)
+        e = group ? launch_stream<1>(a, st) : launch_stream<0>(a, st);
+    else
+        e = launch_gemm_experts(a, form == 2 ? 64 : form == 3 ? 128 : 0, st);
     return e == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+}  // namespace flexq
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+flexq_status flexq_expert_linear(const void *packed, int E, int group, const int8_t *xq, const uint16_t *sx, int x_rows,
+                                 const int32_t *order, const int32_t *offsets, int slots, int k, int scatter, int N,
+                                 int K, uint16_t *y, void *stream)
+{
+    return flexq::expert_impl(0, packed, E, group, xq, sx, x_rows, order, offsets, slots, k, scatter, N, K, y, stream, nullptr);
 }
 
 flexq_status flexq_expert_combine(const uint16_t *y, const int32_t *experts, const float *weights, const uint16_t *add,

@@ -64,6 +64,14 @@ struct LinearArgs {
                              // are resident together; when they are not, a short bound costs the least
 };
 
+// The same for rows grouped by expert: packed is expert 0's, M is not used, one K split.
+struct ExpertLinear : LinearArgs {
+    size_t expert_bytes;         // from one expert's packed weights to the next one's
+    const int32_t *order, *offsets;
+    int E, slots, x_rows, k;     // k: slots of a token's row of x; 0: rows of x are sorted rows
+    int scatter;                 // output row order[r] instead of r
+};
+
 hipError_t launch_quant_w6(const float *w, int N, int K, int group, int8_t *wq, uint16_t *sw,
                            hipStream_t st);
 // `layout` 0 writes the codes row-major; layout == act_bits writes them in tile order for
@@ -106,6 +114,8 @@ bool skinny_slice_fits(int M, int K, int split_k);
 // 256x256 form, the number of runs its tail was cut into.
 hipError_t launch_gemm(const LinearArgs &a, int cfg, hipStream_t st, int *chosen = nullptr,
                        int *tail_runs = nullptr);
+// The experts' layers on tiles of that many rows (64, 128; 256 columns wide: 0) of one expert.
+hipError_t launch_gemm_experts(const ExpertLinear &a, int rows, hipStream_t st);
 // 256-row tiles with both operands through LDS: per-channel scales, no K split.  The
 // tiles beyond the last whole round of 256 ("the tail") run in one of three forms:
 // tail_form 0: as whole 256x256 tiles; 1: as twice as many 256x128 tiles; 2: cut along K

@@ -26,13 +26,22 @@
 #include "flexq_device.h"
 #include "flexq_kernels.h"
 #include "gemm_common.h"
+#include "row_groups.h"
 #include <type_traits>
 
 namespace {
 
-template <int WM, int WN, int MT, int NT, int GROUP, int WPE>
+__device__ __forceinline__ int expert_x_rows(const flexq::LinearArgs &a) { return a.M; }
+__device__ __forceinline__ int expert_x_rows(const flexq::ExpertLinear &a) { return a.x_rows; }
+
+
+// Args: LinearArgs, or ExpertLinear for rows grouped by expert.  There a tile is rows of one expert (tiles
+// begin anew with each), its rows of x are gathered -- the DMA takes an address per lane, so this costs
+// nothing but the look-up ahead of the first stage -- and its rows of y may be scattered; the tile count
+// is known on the device only, so the grid is an upper bound and every workgroup finds its place.
+template <int WM, int WN, int MT, int NT, int GROUP, int WPE, class Args>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
-void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
+void gemm_kernel(Args a, int tiles_m, int tiles_n)
 {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer-resource builtins exist in the device pass only
     constexpr int WAVES = WM * WN;
@@ -48,17 +57,22 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int M = a.M, N = a.N, K = a.K;
+    constexpr bool EXPERTS = !std::is_same<Args, flexq::LinearArgs>::value;
+    static_assert(!EXPERTS || GROUP != 2, "experts take one scale per token");
+    int M = a.M;
+    const int N = a.N, K = a.K;
     const int KT = K / FLEXQ_TILE_K;
 
     // ---- XCD-aware tile choice: blocks 8 apart share an XCD ---------------
     // K splits of one output tile are adjacent block ids
-    const int KS = a.split_k;
+    const int KS = EXPERTS ? 1 : a.split_k;
     const int ksplit = blockIdx.x % KS;
     const int kb0 = (int)((long)ksplit * KT / KS);              // first 128-k stage of this block
     const int KN = (int)((long)(ksplit + 1) * KT / KS) - kb0;   // and how many
+    if constexpr (EXPERTS) tiles_m = count_pieces(a.offsets, a.E, a.slots, BM);
     const int nblk = tiles_m * tiles_n;
     int bid = blockIdx.x / KS;
+    if (EXPERTS && bid >= nblk) return;
     const int tile_id = bid;
     {
         const int per = nblk / 8, rem = nblk % 8;
@@ -73,7 +87,29 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
     const int in_sup = bid - sup * SUP_M * tiles_n;
     const int tile_m = first_m + in_sup % span_m;
     const int tile_n = in_sup / span_m;
-    const int bm0 = tile_m * BM, bn0 = tile_n * BN;
+    int bm0 = tile_m * BM;
+    const int bn0 = tile_n * BN;
+    // rows of x and y and token scales of the tile, behind the stage buffers
+    int *const in_row = reinterpret_cast<int *>(lds + 3 * XSTAGE), *const out_row = in_row + BM;
+    float *const row_sx = reinterpret_cast<float *>(out_row + BM);
+    const uint8_t *packed = static_cast<const uint8_t *>(a.packed);
+    const uint16_t *scales = a.scales;
+    if constexpr (EXPERTS) {
+        const RowGroup g = find_piece(a.offsets, a.E, a.slots, BM, tile_m);
+        bm0 = g.begin + BM * g.tile;
+        M = g.end;
+        packed += (size_t)g.id * a.expert_bytes;
+        scales = reinterpret_cast<const uint16_t *>(packed + (size_t)N * K / 4 * 3);
+        for (int i = tid; i < BM; i += 64 * WAVES) {
+            const int r = min(bm0 + i, M - 1);           // rows beyond the expert's last repeat it and are not stored
+            const int slot = min(max(a.order[r], 0), a.slots - 1);
+            const int in = a.k ? min(slot / a.k, a.x_rows - 1) : r;
+            in_row[i] = in;
+            out_row[i] = a.scatter ? slot : r;
+            row_sx[i] = h2f(a.sx[in]);
+        }
+        lds_barrier();
+    }
 
     // ---- activations: global -> LDS by DMA, no registers in between --------
     // DMA load q of a stage fills LDS bytes [1024q, 1024q + 1024) = rows 8q..8q+7;
@@ -83,14 +119,14 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
     // unit: a lane's offset is fixed for the whole kernel, the k offset is an
     // SGPR, and rows beyond M fall outside the buffer and read as zero.
     const __amdgpu_buffer_rsrc_t xrsrc = __builtin_amdgcn_make_buffer_rsrc(
-        (void *)a.xq, 0, (unsigned)((long)M * K), 0x00020000);
+        (void *)a.xq, 0, (unsigned)((long)(EXPERTS ? expert_x_rows(a) : M) * K), 0x00020000);
     unsigned xoff[XDMA];
 #pragma unroll
     for (int i = 0; i < XDMA; ++i) {
         const int q = wave * XDMA + i;
         const int row = 8 * q + (lane >> 3);
         const int c = (lane & 7) ^ ((row >> 1) & 7);
-        xoff[i] = (unsigned)(bm0 + row) * (unsigned)K + 16u * c;
+        xoff[i] = (unsigned)(EXPERTS ? in_row[row] : bm0 + row) * (unsigned)K + 16u * c;
     }
     auto dma_x = [&](int kb, int buf) {
 #pragma unroll
@@ -104,7 +140,7 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
 
     // ---- per-wave packed tiles: SGPR tile offset + lane * 16 -----------------
     const __amdgpu_buffer_rsrc_t wrsrc = __builtin_amdgcn_make_buffer_rsrc(
-        (void *)a.packed, 0, (unsigned)((long)N * K / 4 * 3), 0x00020000);
+        (void *)packed, 0, (unsigned)((long)N * K / 4 * 3), 0x00020000);
     bool wvalid[NT];
     int wnb[NT];
 #pragma unroll
@@ -181,7 +217,7 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
             wreg[B][nt].q0 = (v4i)__builtin_amdgcn_raw_buffer_load_b128(wrsrc, wlane, soff, 0);
             wreg[B][nt].q1 = (v4i)__builtin_amdgcn_raw_buffer_load_b128(wrsrc, wlane, soff + 1024, 0);
             wreg[B][nt].q2 = (v4i)__builtin_amdgcn_raw_buffer_load_b128(wrsrc, wlane, soff + 2048, 0);
-            if (GROUP) gsreg[B][nt] = a.scales[((long)wnb[nt] * KT + kb0 + kb) * 32 + (lane & 31)];
+            if (GROUP) gsreg[B][nt] = scales[((long)wnb[nt] * KT + kb0 + kb) * 32 + (lane & 31)];
         }
     };
 
@@ -413,7 +449,7 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
     const bool cvalid = n_lane < N;
     float swv[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) swv[c] = GROUP ? 0.25f : h2f(a.scales[cvalid ? n_lane + c : 0]);
+    for (int c = 0; c < 4; ++c) swv[c] = GROUP ? 0.25f : h2f(scales[cvalid ? n_lane + c : 0]);
     // scale and store four columns of row m (q: exact int32 sums, or fp32 group sums)
     auto finish = [&](const v4i &q, int m, float sxm) {
         uint16_t h[4];
@@ -423,8 +459,8 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
         uint2 out2;
         out2.x = (unsigned)h[0] | ((unsigned)h[1] << 16);
         out2.y = (unsigned)h[2] | ((unsigned)h[3] << 16);
-        *reinterpret_cast<uint2 *>(a.y + (long)m * N + n_lane) = out2;
-        if (!GROUP && a.acc_out) *reinterpret_cast<v4i *>(a.acc_out + (long)m * N + n_lane) = q;
+        *reinterpret_cast<uint2 *>(a.y + (long)(EXPERTS ? out_row[m - bm0] : m) * N + n_lane) = out2;
+        if (!GROUP && !EXPERTS && a.acc_out) *reinterpret_cast<v4i *>(a.acc_out + (long)m * N + n_lane) = q;
     };
     // split-K partial sums [split][M][N] int32, addressed as a buffer; cache policy
     // bit 4 = sc1 = device scope: the access goes to memory all XCDs share
@@ -441,7 +477,10 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
         for (int i = 0; i < 32 / RPI; ++i) {
             const int m = bm0 + (wm * MT + mt) * 32 + i * RPI + erow;
             // (mode 2 is scaled per group already; K splits scale after they have met)
-            sxall[mt][i] = (GROUP != 2 && KS == 1 && m < M) ? h2f(a.sx[m]) : 1.0f;
+            if constexpr (EXPERTS)
+                sxall[mt][i] = row_sx[m - bm0];
+            else
+                sxall[mt][i] = (GROUP != 2 && KS == 1 && m < M) ? h2f(a.sx[m]) : 1.0f;
         }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -475,7 +514,7 @@ void gemm_kernel(flexq::LinearArgs a, int tiles_m, int tiles_n)
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // reads done before the next slab overwrites
     }
-    if (KS == 1) return;
+    if (EXPERTS || KS == 1) return;
 
     // ---- K splits meet: the last block of this tile to arrive adds the partial
     // sums in split order and stores the tile.  Partial sums were written with
@@ -565,7 +604,7 @@ hipError_t launch_cfg(const flexq::LinearArgs &a, hipStream_t st)
     constexpr int BM = WM * MT * 32, BN = WN * NT * 32;
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
     const size_t lds_bytes = 3 * BM * 128 + (GROUP == 2 ? 4 * BM * 2 : 0);
-    auto kern = gemm_kernel<WM, WN, MT, NT, GROUP, WPE>;
+    auto kern = gemm_kernel<WM, WN, MT, NT, GROUP, WPE, flexq::LinearArgs>;
     static std::atomic<unsigned long long> lds_allowed{0};
     if (hipError_t e = flexq::allow_dynamic_lds(reinterpret_cast<const void *>(kern), (int)lds_bytes, lds_allowed);
         e != hipSuccess)
@@ -576,9 +615,33 @@ hipError_t launch_cfg(const flexq::LinearArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int WM, int WN, int MT, int NT, int GROUP, int WPE>
+hipError_t launch_experts_cfg(const flexq::ExpertLinear &a, hipStream_t st)
+{
+    constexpr int BM = WM * MT * 32, BN = WN * NT * 32;
+    // every expert may end in a tile of its own
+    const long tiles_m = a.slots / BM + (a.E < a.slots ? a.E : a.slots), tiles_n = (a.N + BN - 1) / BN;
+    if (tiles_m * tiles_n >= (1L << 31)) return hipErrorInvalidValue;
+    const size_t lds_bytes = 3 * BM * 128 + 3 * BM * 4;
+    auto kern = gemm_kernel<WM, WN, MT, NT, GROUP, WPE, flexq::ExpertLinear>;
+    static std::atomic<unsigned long long> lds_allowed{0};
+    if (hipError_t e = flexq::allow_dynamic_lds(reinterpret_cast<const void *>(kern), (int)lds_bytes, lds_allowed);
+        e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WM * WN), lds_bytes, st, a, 0, (int)tiles_n);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 namespace flexq {
+
+hipError_t launch_gemm_experts(const ExpertLinear &a, int rows, hipStream_t st)
+{
+    if (a.group != 0) return rows == 64 ? launch_experts_cfg<1, 4, 2, 1, 1, 2>(a, st) : launch_experts_cfg<1, 4, 4, 1, 1, 2>(a, st);
+    if (rows == 64) return launch_experts_cfg<1, 4, 2, 1, 0, 4>(a, st);
+    return rows == 128 ? launch_experts_cfg<1, 4, 4, 1, 0, 3>(a, st) : launch_experts_cfg<1, 4, 4, 2, 0, 2>(a, st);
+}
 
 hipError_t launch_gemm(const LinearArgs &a, int cfg, hipStream_t st, int *chosen, int *tail_runs)
 {

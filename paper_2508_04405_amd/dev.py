@@ -41,6 +41,9 @@ def load():
     lib.flexq_dev_layer_linears.restype = c_int
     lib.flexq_dev_layer_linears.argtypes = [ctypes.POINTER(Tuning), vp, c_int, vp, c_int, c_int, vp, c_size, vp,
                                             ctypes.POINTER(c_int)]
+    lib.flexq_dev_expert_linear.restype = c_int
+    lib.flexq_dev_expert_linear.argtypes = [c_int, vp, c_int, c_int, vp, vp, c_int, vp, vp, c_int, c_int, c_int, c_int,
+                                            c_int, vp, vp, ctypes.POINTER(c_int)]
     lib.flexq_dev_probe_hbm_read.restype = c_int
     lib.flexq_dev_probe_hbm_read.argtypes = [vp, c_size, vp, vp]
     lib.flexq_dev_probe_mfma_i8.restype = c_int
@@ -161,3 +164,14 @@ def probe_mfma_mix(a_operands, b_operands, valu_per_mfma, lds_reads_per_8, iters
     assert b_operands.numel() * b_operands.element_size() >= 16384
     _check(load().flexq_dev_probe_mfma_mix(_ptr(a_operands), _ptr(b_operands), valu_per_mfma, lds_reads_per_8,
                                            iters, workgroups, waves, _ptr(sink), _stream()))
+
+
+def expert_linear(form, packed, N, K, xq, sx, order, offsets, group=0, k=0, scatter=False, out=None):
+    """binding.expert_linear with a forced kernel -> (y, the form that ran)."""
+    E, slots = packed.shape[0], order.numel()
+    y = out if out is not None else torch.empty((slots, N), dtype=torch.float16, device=xq.device)
+    got = ctypes.c_int(0)
+    _check(load().flexq_dev_expert_linear(form, _ptr(packed), E, group, _ptr(xq), _ptr(sx), xq.shape[0], _ptr(order),
+                                          _ptr(offsets), slots, k, int(bool(scatter)), N, K, _ptr(y), _stream(),
+                                          ctypes.byref(got)))
+    return y, got.value

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2508_04405_amd as fq
+from paper_2508_04405_amd import dev
 import rows_reference as ref
 from gpu_helpers import assert_y_close, say, to_dev
 
@@ -152,17 +153,22 @@ def check_experts(rng, M, E, k, N, K, group, bits, experts, sorted_rows=False, s
     xq, sx = draw_rows(rng, M * k if sorted_rows else M, K, bits)
     packed = fq.pack_experts(to_dev(codes), to_dev(sw), group)
     order, offsets = ref.group_rows(experts, E)
-    out = torch.full((M * k, N), 7.0, dtype=torch.float16, device=DEV)
-    fq.expert_linear(packed, N, K, to_dev(xq), to_dev(sx), to_dev(order), to_dev(offsets), group=group,
-                     k=0 if sorted_rows else k, scatter=scatter, out=out)
+    args = (packed, N, K, to_dev(xq), to_dev(sx), to_dev(order), to_dev(offsets))
+    kw = dict(group=group, k=0 if sorted_rows else k, scatter=scatter)
     total = int(offsets[-1])
     want, slack = ref.expert_rows(codes, sw, xq, sx, order, offsets, 0 if sorted_rows else k, group)
-    got = host(out)
     rows = order[:total] if scatter else np.arange(total)
-    if total:
-        assert_y_close(got[rows], want.astype(np.float16), slack if group else None)
     rest = np.setdiff1d(np.arange(M * k), rows)
-    assert np.all(got[rest] == 7.0), "rows without an expert are left as they were"
+    for form in range(5):                                     # the library's choice, then every kernel
+        out = torch.full((M * k, N), 7.0, dtype=torch.float16, device=DEV)
+        if form == 0:
+            fq.expert_linear(*args, out=out, **kw)
+        else:
+            dev.expert_linear(form, *args, out=out, **kw)
+        got = host(out)
+        if total:
+            assert_y_close(got[rows], want.astype(np.float16), slack if group else None)
+        assert np.all(got[rest] == 7.0), "rows without an expert are left as they were"
 
 
 def some_experts(rng, M, E, k, dropped=0.0):
