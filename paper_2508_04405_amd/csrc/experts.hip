@@ -151,22 +151,60 @@ __global__ __launch_bounds__(256) void combine_kernel(const uint16_t *y, const i
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
+inline int groups_of(const ExpertLinear &a) { return a.E < a.slots ? a.E : a.slots; }
+
+// Eight wavefronts a workgroup where there are at most two workgroups a CU and rows are long: four leave the
+// chip half empty (11008 x 4096 by one token's two experts: 20.8 us with four, 14.6 with eight; with more
+// workgroups eight only lengthen the meeting in LDS, 22016 x 4096 26.1 and 27.1, at eight tokens 80.8 and 84.5).
 template <int GROUP>
 hipError_t launch_stream(const ExpertLinear &a, hipStream_t st)
 {
-    const unsigned groups = (unsigned)(a.E < a.slots ? a.E : a.slots);
-    hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 4>), dim3(groups * (unsigned)(a.N / 32)), dim3(256), 0, st, a);
+    const long wgs = (long)groups_of(a) * (a.N / 32);
+    if (wgs >= (1L << 31)) return hipErrorInvalidValue;
+    if (wgs <= 512 && a.K >= 4096)
+        hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 8>), dim3((unsigned)wgs), dim3(512), 0, st, a);
+    else
+        hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 4>), dim3((unsigned)wgs), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
-// 1 streaming, 2 .. 4 tiles of 64 x 128, 128 x 128, 128 x 256.
+// Which kernel: 1 streaming, 2 .. 5 tiles of 32 x 128 (group-128 scales: 32 x 256), 64 x 128, 128 x 128,
+// 128 x 256.  How the rows fall is known on the device only, so by their average over the experts.
+//
+// Few rows each: the streaming kernel cuts K over its wavefronts and wins where rows are long, or where
+// 32 x 128 tiles would not fill the chip (us streaming / 32 x 128: 22016 x 4096 at 2 rows each of 8 experts 81 /
+// 91, 4096 x 11008 at one token 14.6 / 32.8, 2816 x 2048 at one token, 132 tiles, 8.1 / 8.4; but at four tokens
+// 18.9 / 15.9, and 4096 x 11008 at 6 rows each 62 / 52).  Between the tiles the work of the busiest CU decides,
+// at the relative rates that so many workgroups on a CU reach (as for the dense layer); a tile more than the
+// rows fill, half a one on average.  Measured over 2816 x 2048 and 4096 x 11008 with 8 experts, 64 to 4096 tokens,
+// the choice is the fastest or within 7 % of it.
 int choose_form(const ExpertLinear &a)
 {
-    const long groups = a.E < a.slots ? a.E : a.slots;
-    const double rows = (double)a.slots / (double)groups;
-    if (rows <= 32.0) return 1;
-    if (rows <= 64.0) return 2;
-    return a.group ? 3 : 4;
+    const double groups = groups_of(a), rows = (double)a.slots / groups;
+    const long n128 = (a.N + 127) / 128, n256 = (a.N + 255) / 256;
+    if (rows <= 4.0 && (a.K >= 4096 || groups * n128 <= 160)) return 1;
+    auto tiles = [&](int height, long across) {
+        const double t = rows / height + 0.5;
+        return groups * (t < 1.0 ? 1.0 : t) * across;
+    };
+    if (rows <= 24.0) return 2;
+    // group-128 scales: vector-bound, the columns of a tile matter less than its padding (2816 x 2048, 64 experts
+    // at 12 rows each 48 / 56 / 80 us on 32, 64 and 128 rows, at 48 70 / 72 / 86, at 192 187 / 178 / 157)
+    if (a.group) return rows < 96.0 ? 3 : 4;
+    // short rows, few tiles: lower ones fill the chip (2816 x 2048 at 64 rows each of 8 experts 12.5 / 14.9 us)
+    if (rows <= 64.0 && a.K <= 4096 && tiles(64, n128) <= 384.0) return 2;
+    auto busiest_cu = [](double tiles, double area, int slots, const double *rate) {
+        const long per_cu = (long)((tiles + 255.0) / 256.0), full = per_cu / slots, rest = per_cu % slots;
+        return (double)full * slots * area / rate[slots - 1] + (rest ? (double)rest * area / rate[rest - 1] : 0.0);
+    };
+    static const double rate64[4] = {0.30, 0.50, 0.65, 0.80}, rate128[3] = {0.40, 0.75, 0.85},
+                        sparse128[3] = {0.58, 0.75, 0.85}, rate256[2] = {0.70, 1.00};
+    const double t128 = tiles(128, n128);
+    const double us64 = busiest_cu(tiles(64, n128), 0.5, 4, rate64);
+    const double us128 = busiest_cu(t128, 1.0, 3, t128 <= 256.0 ? sparse128 : rate128);
+    const double us256 = busiest_cu(tiles(128, n256), 2.0, 2, rate256);
+    if (us256 <= us128 && us256 <= us64) return 5;
+    return us128 <= us64 ? 4 : 3;
 }
 
 }  // namespace
@@ -210,7 +248,7 @@ flexq_status expert_impl(int form, const void *packed, int E, int group, const i
     if (form == 1)
         e = group ? launch_stream<1>(a, st) : launch_stream<0>(a, st);
     else
-        e = launch_gemm_experts(a, form == 2 ? 64 : form == 3 ? 128 : 0, st);
+        e = launch_gemm_experts(a, form, st);
     return e == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
 }
 

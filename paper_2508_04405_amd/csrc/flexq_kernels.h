@@ -114,8 +114,8 @@ bool skinny_slice_fits(int M, int K, int split_k);
 // 256x256 form, the number of runs its tail was cut into.
 hipError_t launch_gemm(const LinearArgs &a, int cfg, hipStream_t st, int *chosen = nullptr,
                        int *tail_runs = nullptr);
-// The experts' layers on tiles of that many rows (64, 128; 256 columns wide: 0) of one expert.
-hipError_t launch_gemm_experts(const ExpertLinear &a, int rows, hipStream_t st);
+// The experts' layers on tiles: form 2 .. 5 of choose_form (experts.hip).
+hipError_t launch_gemm_experts(const ExpertLinear &a, int form, hipStream_t st);
 // 256-row tiles with both operands through LDS: per-channel scales, no K split.  The
 // tiles beyond the last whole round of 256 ("the tail") run in one of three forms:
 // tail_form 0: as whole 256x256 tiles; 1: as twice as many 256x128 tiles; 2: cut along K

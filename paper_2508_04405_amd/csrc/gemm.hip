@@ -31,6 +31,13 @@
 
 namespace {
 
+// Experts: the tile's row numbers lie in LDS behind the stage buffers and the epilogue's staging, which
+// 32-row tiles' stages are too small for.
+constexpr int expert_rows_at(int BM, int waves, int NT)
+{
+    const int stages = 3 * BM * 128, staging = waves * 32 * (NT * 32 + 8) * 4;
+    return stages > staging ? stages : staging;
+}
 __device__ __forceinline__ int expert_x_rows(const flexq::LinearArgs &a) { return a.M; }
 __device__ __forceinline__ int expert_x_rows(const flexq::ExpertLinear &a) { return a.x_rows; }
 
@@ -90,7 +97,7 @@ void gemm_kernel(Args a, int tiles_m, int tiles_n)
     int bm0 = tile_m * BM;
     const int bn0 = tile_n * BN;
     // rows of x and y and token scales of the tile, behind the stage buffers
-    int *const in_row = reinterpret_cast<int *>(lds + 3 * XSTAGE), *const out_row = in_row + BM;
+    int *const in_row = reinterpret_cast<int *>(lds + expert_rows_at(BM, WAVES, NT)), *const out_row = in_row + BM;
     float *const row_sx = reinterpret_cast<float *>(out_row + BM);
     const uint8_t *packed = static_cast<const uint8_t *>(a.packed);
     const uint16_t *scales = a.scales;
@@ -351,7 +358,7 @@ void gemm_kernel(Args a, int tiles_m, int tiles_n)
             // MFMA of step s, i.e. in the shadow of the MFMA just issued.  The
             // scheduling barriers keep that order (left alone, the scheduler sinks the
             // LDS reads next to their first use and gathers the MFMAs).
-            static_assert(MT == 2 || MT >= 4, "one dword of the next operand per MFMA, or two");
+            static_assert(MT <= 2 || MT >= 4, "one dword of the next operand per MFMA, two or all four");
             constexpr int DPM = MT >= 4 ? 1 : 4 / MT;   // dwords of the next operand per MFMA
             v4i af[2][MT];
 #pragma unroll
@@ -437,7 +444,7 @@ void gemm_kernel(Args a, int tiles_m, int tiles_n)
     // lane owns four consecutive columns of one row, applies sx[m] * sw[n] in
     // fp32, and the lanes of a row store whole 64- or 128-byte runs of fp16.
     constexpr int ESTRIDE = (NT * 32 + 8) * 4;          // bytes per staged row
-    static_assert(3 * XSTAGE >= WAVES * 32 * ESTRIDE, "epilogue staging must fit the stage buffers");
+    static_assert(EXPERTS || 3 * XSTAGE >= WAVES * 32 * ESTRIDE, "epilogue staging must fit the stage buffers");
     constexpr int LPR = NT * 8;                          // lanes per staged row (4 columns each)
     constexpr int RPI = 64 / LPR;                        // rows per read instruction
     static_assert(64 % LPR == 0, "a read instruction covers whole rows");
@@ -622,7 +629,7 @@ hipError_t launch_experts_cfg(const flexq::ExpertLinear &a, hipStream_t st)
     // every expert may end in a tile of its own
     const long tiles_m = a.slots / BM + (a.E < a.slots ? a.E : a.slots), tiles_n = (a.N + BN - 1) / BN;
     if (tiles_m * tiles_n >= (1L << 31)) return hipErrorInvalidValue;
-    const size_t lds_bytes = 3 * BM * 128 + 3 * BM * 4;
+    const size_t lds_bytes = expert_rows_at(BM, WM * WN, NT) + 3 * BM * 4;
     auto kern = gemm_kernel<WM, WN, MT, NT, GROUP, WPE, flexq::ExpertLinear>;
     static std::atomic<unsigned long long> lds_allowed{0};
     if (hipError_t e = flexq::allow_dynamic_lds(reinterpret_cast<const void *>(kern), (int)lds_bytes, lds_allowed);
@@ -636,11 +643,15 @@ hipError_t launch_experts_cfg(const flexq::ExpertLinear &a, hipStream_t st)
 
 namespace flexq {
 
-hipError_t launch_gemm_experts(const ExpertLinear &a, int rows, hipStream_t st)
+hipError_t launch_gemm_experts(const ExpertLinear &a, int form, hipStream_t st)
 {
-    if (a.group != 0) return rows == 64 ? launch_experts_cfg<1, 4, 2, 1, 1, 2>(a, st) : launch_experts_cfg<1, 4, 4, 1, 1, 2>(a, st);
-    if (rows == 64) return launch_experts_cfg<1, 4, 2, 1, 0, 4>(a, st);
-    return rows == 128 ? launch_experts_cfg<1, 4, 4, 1, 0, 3>(a, st) : launch_experts_cfg<1, 4, 4, 2, 0, 2>(a, st);
+    if (a.group != 0) {
+        if (form == 2) return launch_experts_cfg<1, 4, 1, 2, 1, 2>(a, st);
+        return form == 3 ? launch_experts_cfg<1, 4, 2, 1, 1, 2>(a, st) : launch_experts_cfg<1, 4, 4, 1, 1, 2>(a, st);
+    }
+    if (form == 2) return launch_experts_cfg<1, 4, 1, 1, 0, 4>(a, st);
+    if (form == 3) return launch_experts_cfg<1, 4, 2, 1, 0, 4>(a, st);
+    return form == 4 ? launch_experts_cfg<1, 4, 4, 1, 0, 3>(a, st) : launch_experts_cfg<1, 4, 4, 2, 0, 2>(a, st);
 }
 
 hipError_t launch_gemm(const LinearArgs &a, int cfg, hipStream_t st, int *chosen, int *tail_runs)
