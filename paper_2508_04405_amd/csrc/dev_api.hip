@@ -58,7 +58,7 @@ flexq_status flexq_dev_expert_linear(int form, const void *packed, int E, int gr
                                      int x_rows, const int32_t *order, const int32_t *offsets, int slots, int k,
                                      int scatter, int N, int K, uint16_t *y, void *stream, int *dispatched)
 {
-    if (form < 0 || form > 5) return FLEXQ_EINVAL;
+    if (form < 0 || form > 6) return FLEXQ_EINVAL;
     return flexq::expert_impl(form, packed, E, group, xq, sx, x_rows, order, offsets, slots, k, scatter, N, K, y, stream,
                               dispatched);
 }

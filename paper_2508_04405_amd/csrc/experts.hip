@@ -247,6 +247,8 @@ flexq_status expert_impl(int form, const void *packed, int E, int group, const i
     hipError_t e;
     if (form == 1)
         e = group ? launch_stream<1>(a, st) : launch_stream<0>(a, st);
+    else if (form == 6)
+        e = launch_expert_tiles(a, st);
     else
         e = launch_gemm_experts(a, form, st);
     return e == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;

@@ -116,6 +116,9 @@ hipError_t launch_gemm(const LinearArgs &a, int cfg, hipStream_t st, int *chosen
                        int *tail_runs = nullptr);
 // The experts' layers on tiles: form 2 .. 5 of choose_form (experts.hip).
 hipError_t launch_gemm_experts(const ExpertLinear &a, int form, hipStream_t st);
+// The same on persistent workgroups, both operands through LDS: 256 x 256 tiles and 128 x 256 ones for what is
+// left of an expert's rows (group-128 scales: 128 x 256 and 64 x 256).
+hipError_t launch_expert_tiles(const ExpertLinear &a, hipStream_t st);
 // 256-row tiles with both operands through LDS: per-channel scales, no K split.  The
 // tiles beyond the last whole round of 256 ("the tail") run in one of three forms:
 // tail_form 0: as whole 256x256 tiles; 1: as twice as many 256x128 tiles; 2: cut along K

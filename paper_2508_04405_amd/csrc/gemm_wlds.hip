@@ -82,9 +82,11 @@
 // above 128 tokens where they fill the chip more evenly than 256-row tiles
 // (gemm_low_choose), those beyond the last whole round cut evenly.  And 192-row tiles, 192x256,
 // whole, where their height fits the tokens or the rounds better (gemm_192_us).
+#include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
 #include "gemm_common.h"
+#include "row_groups.h"
 #include <type_traits>
 
 namespace {
@@ -164,6 +166,17 @@ struct Shape {
     static constexpr int LDS_BYTES = GROUPED ? SF32 + BN * 4 : SRING;
     static_assert(LDS_BYTES + 1024 <= 160 * 1024, "LDS of one CU (plus the static part)");
 };
+
+// Experts: the tables of ExpertWalk lie behind both phases' shapes (516 offsets, 1024 row numbers).
+template <int GROUP>
+constexpr int kExpertTables = GROUP ? (Shape<4>::LDS_BYTES > Shape<5>::LDS_BYTES ? Shape<4>::LDS_BYTES : Shape<5>::LDS_BYTES)
+                                    : (Shape<2>::LDS_BYTES > Shape<3>::LDS_BYTES ? Shape<2>::LDS_BYTES : Shape<3>::LDS_BYTES);
+template <int GROUP>
+constexpr int kExpertLds = kExpertTables<GROUP> + (516 + 1024) * 4;
+static_assert(kExpertLds<0> + 1024 <= 160 * 1024 && kExpertLds<1> + 1024 <= 160 * 1024, "LDS of one CU");
+
+__device__ __forceinline__ int x_rows_of(const flexq::LinearArgs &a) { return a.M; }
+__device__ __forceinline__ int x_rows_of(const flexq::ExpertLinear &a) { return a.x_rows; }
 
 // One item of a workgroup's list: stages [ks, ke) of the 256-wide tile `t256`
 // (its half `half` when the items are half tiles); `tj` numbers the tile within a cut tail.
@@ -407,6 +420,15 @@ __device__ __forceinline__ void group_item(v16f (&facc)[Shape<TILE>::MT][1], uin
     }
 }
 
+// Rows grouped by expert: what a phase of a launch needs beside its arguments.  Each expert's rows are cut
+// into tiles of `high` rows and a last one, which is `high` too if it holds more than `low`: those are phase 0;
+// the other last ones run as tiles of `low` rows in phase 1.
+struct ExpertWalk {
+    const int *offsets;      // LDS: offsets[0 .. E]
+    int *rows;               // LDS, [2][2][256]: rows of x and of y of the item at hand, and of the next one
+    int phase, rotate;       // rotate: this phase's items begin at that workgroup of every XCD
+};
+
 // One phase of a launch: this workgroup's share of `item_count` items that begin at the
 // 256-wide tile `item_begin` -- whole tiles (TILE = 2), half tiles (two items per tile),
 // or, with SK, the stages of `item_count` tiles cut into `tail_wgs` runs.
@@ -414,9 +436,12 @@ __device__ __forceinline__ void group_item(v16f (&facc)[Shape<TILE>::MT][1], uin
 // operands' scales per group.
 // YPOLICY, WPOLICY: cache policies of the outputs' stores and of the weights' DMA loads (the latter
 // with per-channel scales).
-template <int TILE, int SK, int GROUP = 0, int YPOLICY = 0, int WPOLICY = 0>
-__device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *lds, int &s_last, int tiles_m,
-                                          int tiles_n, int item_begin, int item_count, int tail_wgs)
+// Args: LinearArgs, or ExpertLinear for rows grouped by expert (whole items only): the rows of x are
+// gathered by the DMA's address per lane, the rows of y may be scattered.
+template <int TILE, int SK, int GROUP = 0, int YPOLICY = 0, int WPOLICY = 0, class Args = flexq::LinearArgs>
+__device__ __forceinline__ void run_items(const Args &a, uint8_t *lds, int &s_last, int tiles_m,
+                                          int tiles_n, int item_begin, int item_count, int tail_wgs,
+                                          const ExpertWalk &walk = {})
 {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer-resource builtins exist in the device pass only
     using S = Shape<TILE>;
@@ -430,6 +455,8 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
+    constexpr bool EXPERTS = !std::is_same<Args, flexq::LinearArgs>::value;
+    static_assert(!EXPERTS || (SK == 0 && GROUP != 2 && S::BM <= 256), "experts: whole items, one scale per token");
     const int M = a.M, N = a.N, K = a.K;
     const int KT = K / FLEXQ_TILE_K;
 
@@ -446,6 +473,10 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     if (!SK) {
         j_next = (int)((long)xcd * item_count / 8) + slot;
         j_end = (int)((long)(xcd + 1) * item_count / 8);
+        if constexpr (EXPERTS) {             // first those workgroups that the phase before left a round short
+            int turned = slot - walk.rotate % (G / 8);
+            j_next += (turned < 0 ? turned + G / 8 : turned) - slot;
+        }
     } else if (SK == 3) {
         // an XCD's tiles, twice: their first pieces among its first workgroups, `tail_wgs` & 255 each,
         // their second pieces among the next ones, tail_wgs >> 8 each
@@ -500,8 +531,8 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     };
 
     const __amdgpu_buffer_rsrc_t xrsrc = __builtin_amdgcn_make_buffer_rsrc(
-        (void *)a.xq, 0, (unsigned)((long)M * K), 0x00020000);
-    const __amdgpu_buffer_rsrc_t wrsrc = __builtin_amdgcn_make_buffer_rsrc(
+        (void *)a.xq, 0, (unsigned)((long)(EXPERTS ? x_rows_of(a) : M) * K), 0x00020000);
+    const __amdgpu_buffer_rsrc_t wrsrc = __builtin_amdgcn_make_buffer_rsrc(   // (experts: one of the item's)
         (void *)a.packed, 0, (unsigned)((long)N * K / 4 * 3), 0x00020000);
 
     // ---- where an item's operands are, and the DMA loads of one stage -----------
@@ -511,6 +542,57 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     struct Where {
         int bm0, bn0;
         unsigned xoff[S::XDMA];
+        int end;                             // experts: the rows' end, the weights, a thread's entry of the order
+        const uint8_t *packed;
+        int entry;
+    };
+    auto scales_at = [&](const Where &w) {
+        if constexpr (EXPERTS) return reinterpret_cast<const uint16_t *>(w.packed + (size_t)N * K / 4 * 3);
+        else return a.scales;
+    };
+    struct Ahead {
+        Item item;
+        Where at;
+        bool any;
+    };
+    struct None {
+    };
+    int parity = 0;                          // experts: which half of walk.rows is the current item's
+    // experts: which tile, and a thread's entry of the order; asked for a whole item ahead
+    auto look_up = [&](const Item &it, Where &w) {
+        if constexpr (EXPERTS) {
+            constexpr int SUP_M = GROUP ? 8 : 4;
+            const int bid = it.t256;
+            const int sup = bid / (SUP_M * tiles_n), first_m = sup * SUP_M;
+            const int span_m = min(SUP_M, tiles_m - first_m), in_sup = bid - sup * SUP_M * tiles_n;
+            constexpr int HIGH = GROUP ? 128 : 256;
+            const RowGroup g = find_part<HIGH>(walk.offsets, a.E, walk.phase, first_m + in_sup % span_m);
+            w.bm0 = g.begin;
+            w.end = g.end;
+            w.bn0 = in_sup / span_m * 256;
+            w.packed = static_cast<const uint8_t *>(a.packed) + (size_t)g.id * a.expert_bytes;
+            if (tid < S::BM) w.entry = a.order[min(g.begin + tid, g.end - 1)];
+        }
+    };
+    // experts: the rows of x and y into LDS (rows beyond the last repeat it and are not stored)
+    auto place = [&](Where &w, int half) {
+        if constexpr (EXPERTS) {
+            int *const in_row = walk.rows + half * 512;
+            if (tid < S::BM) {
+                const int r = min(w.bm0 + tid, w.end - 1), slot_row = min(max(w.entry, 0), a.slots - 1);
+                in_row[tid] = a.k ? min((int)((unsigned)slot_row / (unsigned)a.k), a.x_rows - 1) : r;
+                in_row[256 + tid] = a.scatter ? slot_row : r;
+            }
+            lds_barrier();
+            int lane_l = lane;
+            asm volatile("" : "+v"(lane_l));
+#pragma unroll
+            for (int i = 0; i < S::XDMA; ++i) {
+                const int row = 8 * (wave * S::XDMA + i) + (lane_l >> 3);
+                const int c = (lane_l & 7) ^ ((row >> 1) & 7);
+                w.xoff[i] = (unsigned)in_row[row] * (unsigned)K + 16u * c;
+            }
+        }
     };
     auto locate = [&](const Item &it, Where &w) {
         int lane_l = lane;        // (opaque: recomputed per item rather than kept live, see the epilogue)
@@ -548,6 +630,12 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     // are never stored.
     const unsigned wlane = (unsigned)lane * 16u;
     auto dma_w = [&](const Where &w, int ks, int kb, int buf) {
+        const __amdgpu_buffer_rsrc_t wsrc = [&] {
+            if constexpr (EXPERTS)
+                return __builtin_amdgcn_make_buffer_rsrc((void *)w.packed, 0, (unsigned)((long)N * K / 4 * 3), 0x00020000);
+            else
+                return wrsrc;
+        }();
         if constexpr (GROUP != 0) {
             // (whole tiles per wavefront: the planes are immediate offsets of one address)
             if (wave < S::WISSUERS) {
@@ -559,9 +647,9 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
                         (void __attribute__((address_space(3))) *)(lds + S::WBASE + buf * S::WSTAGE +
                                                                    t * FLEXQ_TILE_BYTES);
                     const unsigned soff = (unsigned)(wtile * KT + ks + kb) * FLEXQ_TILE_BYTES;
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wrsrc, dst, 16, wlane, soff, 0, 0);
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wrsrc, dst, 16, wlane, soff, 1024, 0);
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wrsrc, dst, 16, wlane, soff, 2048, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wsrc, dst, 16, wlane, soff, 0, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wsrc, dst, 16, wlane, soff, 1024, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(wsrc, dst, 16, wlane, soff, 2048, 0);
                 }
             }
             return;
@@ -574,7 +662,7 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
                 const int wtile = min(w.bn0 / 32 + t, N / 32 - 1);
                 uint8_t *dst = lds + S::WBASE + buf * S::WSTAGE + p * 1024;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    wrsrc, (void __attribute__((address_space(3))) *)dst, 16, wlane,
+                    wsrc, (void __attribute__((address_space(3))) *)dst, 16, wlane,
                     (unsigned)(wtile * KT + ks + kb) * FLEXQ_TILE_BYTES + 1024u * plane, 0, WPOLICY);
             }
         }
@@ -582,19 +670,25 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     // Group tiles: the stage's scales, two bytes each, by 4-byte DMA loads into a ring of four
     // slots: the eight weight tiles' 32 scales each (wavefronts 4 and 5, four tiles a load)
     // and, with group-wise token scales, the 128 rows' (wavefront 6).
-    const __amdgpu_buffer_rsrc_t srsrc = __builtin_amdgcn_make_buffer_rsrc(
+    const __amdgpu_buffer_rsrc_t srsrc = __builtin_amdgcn_make_buffer_rsrc(    // (experts: one of the item's)
         (void *)a.scales, 0, GROUP ? (unsigned)((long)N * KT * 2) : 0u, 0x00020000);
     const __amdgpu_buffer_rsrc_t xsrsrc = __builtin_amdgcn_make_buffer_rsrc(
         (void *)(GROUP == 2 ? a.sxg : a.scales), 0, GROUP == 2 ? (unsigned)((long)KT * a.sxg_stride * 2) : 0u,
         0x00020000);
     auto dma_s = [&](const Where &w, int ks, int kb) {
         if constexpr (GROUP != 0) {
+            const __amdgpu_buffer_rsrc_t ssrc = [&] {
+                if constexpr (EXPERTS)
+                    return __builtin_amdgcn_make_buffer_rsrc((void *)scales_at(w), 0, (unsigned)((long)N * KT * 2), 0x00020000);
+                else
+                    return srsrc;
+            }();
             uint8_t *slot = lds + S::SRING + (kb & 3) * S::SSLOT;
             if (wave == 4 || wave == 5) {
                 const int t = 4 * (wave - 4) + (lane >> 4);
                 const int wtile = min(w.bn0 / 32 + t, N / 32 - 1);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    srsrc, (void __attribute__((address_space(3))) *)(slot + (wave - 4) * 256), 4,
+                    ssrc, (void __attribute__((address_space(3))) *)(slot + (wave - 4) * 256), 4,
                     (unsigned)wtile * (unsigned)KT * 64u + (unsigned)(lane & 15) * 4u, (unsigned)(ks + kb) * 64u, 0, 0);
             }
             if (GROUP == 2 && wave == 6) {
@@ -627,13 +721,23 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
     Item cur;
     Where at;
     if (!take(cur)) return;
-    locate(cur, at);
+    if constexpr (EXPERTS) {
+        look_up(cur, at);
+        place(at, 0);
+    } else {
+        locate(cur, at);
+    }
     issue_prologue(cur, at);
     wait_vmcnt<0>();
     lds_barrier();
 
     for (;;) {
         const int ks = cur.ks, KN = cur.ke - cur.ks;
+        std::conditional_t<EXPERTS, Ahead, None> ahead;       // experts: the next item, looked up a whole item early
+        if constexpr (EXPERTS) {
+            ahead.any = take(ahead.item);
+            if (ahead.any) look_up(ahead.item, ahead.at);
+        }
 
         // int32 sums of 4 x the product, or (group scales) fp32 sums of the scaled group sums
         std::conditional_t<GROUP != 0, v16f, v16i> acc[MT][NT];
@@ -1204,9 +1308,19 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
         // ---- the next item's first stages set out now, before this tile is stored ----
         Item nxt_item;
         Where nxt_at;
-        const bool has_next = take(nxt_item);
+        bool has_next;
+        if constexpr (EXPERTS) {
+            has_next = ahead.any;
+            nxt_item = ahead.item;
+            nxt_at = ahead.at;
+        } else {
+            has_next = take(nxt_item);
+        }
         if (has_next) {
-            locate(nxt_item, nxt_at);
+            if constexpr (EXPERTS)
+                place(nxt_at, parity ^ 1);
+            else
+                locate(nxt_item, nxt_at);
             issue_prologue(nxt_item, nxt_at);
         }
 
@@ -1235,14 +1349,16 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = n_wave + nt * 32 + 8 * q + 4 * hh;
-                    sw4[nt][q] = cvalid ? *reinterpret_cast<const uint2 *>(a.scales + n) : make_uint2(0u, 0u);
+                    sw4[nt][q] = cvalid ? *reinterpret_cast<const uint2 *>(scales_at(at) + n) : make_uint2(0u, 0u);
                 }
             }
             float sxq[MT];
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int m = bm0 + (wm * MT + mt) * 32 + ml;
-                if (GROUP == 2)
+                if constexpr (EXPERTS)
+                    sxq[mt] = 0.25f * h2f(a.sx[walk.rows[parity * 512 + m - bm0]]);
+                else if (GROUP == 2)
                     sxq[mt] = 0.25f;
                 else
                     sxq[mt] = m < M ? 0.25f * h2f(a.sx[m]) : 0.0f;
@@ -1254,6 +1370,7 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
             const bool ecvalid = n_wave + echunk * 8 < N;
             // the output as a buffer from this wavefront's corner: a lane's offset is fixed,
             // the row offset is an SGPR
+            const int end = EXPERTS ? at.end : M;
             const long corner = (long)(bm0 + wm * MT * 32) * N + n_wave;
             const __amdgpu_buffer_rsrc_t yrsrc = __builtin_amdgcn_make_buffer_rsrc(
                 (void *)(a.y + corner), 0, (unsigned)(((long)(MT * 32 - 1) * N + NT * 32) * 2), 0x00020000);
@@ -1261,7 +1378,7 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int m_slab = bm0 + (wm * MT + mt) * 32;
-                if (m_slab >= M) break;                          // uniform: nothing below is stored
+                if (m_slab >= end) break;                        // uniform: nothing below is stored
                 if (SK == 2 && !((fin_slabs >> mt) & 1u)) continue;   // uniform: another piece stores this slab
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -1279,7 +1396,7 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
                         out2.y = (unsigned)h[2] | ((unsigned)h[3] << 16);
                         *reinterpret_cast<uint2 *>(stg + ml * S::ESTRIDE + (nt * 32 + 8 * q + 4 * hh) * 2) = out2;
                     }
-                if constexpr (!GROUP) {
+                if constexpr (!GROUP && !EXPERTS) {
                     if (a.acc_out) {     // the exact int32 sums, straight from the registers
                         const int m = m_slab + ml;
     #pragma unroll
@@ -1300,7 +1417,12 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
                 for (int i = 0; i < 32 / RPI; ++i) {
                     const int row = i * RPI + erow;
                     const v4u piece = *reinterpret_cast<const v4u *>(stg + row * S::ESTRIDE + echunk * 16);
-                    if (m_slab + row < M && ecvalid)
+                    if constexpr (EXPERTS) {
+                        if (m_slab + row < end && ecvalid) {
+                            const int to = walk.rows[parity * 512 + 256 + m_slab + row - bm0];
+                            *reinterpret_cast<v4u *>(a.y + (size_t)to * N + n_wave + echunk * 8) = piece;
+                        }
+                    } else if (m_slab + row < end && ecvalid)
                         __builtin_amdgcn_raw_buffer_store_b128(piece, yrsrc, yoff,
                                                                (unsigned)((mt * 32 + i * RPI) * N * 2), YPOLICY);
                 }
@@ -1313,8 +1435,34 @@ __device__ __forceinline__ void run_items(const flexq::LinearArgs &a, uint8_t *l
         lds_barrier();
         cur = nxt_item;
         at = nxt_at;
+        parity ^= 1;
     }
 #endif
+}
+
+// Rows grouped by expert: tiles of HIGH rows, then what is left of the experts as tiles of half of that (see
+// ExpertWalk).  How many there are is known here only.
+template <int GROUP>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void gemm_expert_kernel(flexq::ExpertLinear a, int tiles_n)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    __shared__ int s_last;
+    constexpr int HIGH = GROUP ? 128 : 256;
+    int *const offsets = reinterpret_cast<int *>(lds + kExpertTables<GROUP>);
+    for (int e = threadIdx.x; e <= a.E; e += 64 * WAVES) offsets[e] = min(max(a.offsets[e], 0), a.slots);
+    __syncthreads();
+    ExpertWalk walk{offsets, offsets + 516, 0, 0};
+    const int high = count_parts<HIGH>(offsets, a.E, 0), low = count_parts<HIGH>(offsets, a.E, 1);
+    run_items<GROUP ? 4 : 2, 0, GROUP>(a, lds, s_last, high, tiles_n, 0, high * tiles_n, 0, walk);
+    if (low == 0) return;
+#if defined(__HIP_DEVICE_COMPILE__)
+    lds_barrier();     // the last epilogue's staging rows, as above
+#endif
+    const int xcd = (int)(blockIdx.x % 8);
+    walk.phase = 1;
+    walk.rotate = (int)((long)(xcd + 1) * high * tiles_n / 8 - (long)xcd * high * tiles_n / 8);
+    run_items<GROUP ? 5 : 3, 0, GROUP>(a, lds, s_last, low, tiles_n, 0, low * tiles_n, 0, walk);
 }
 
 // ONE_ROUND: no workgroup has more than one item.
@@ -1725,6 +1873,22 @@ hipError_t launch_gemm_group_pairs(const LinearArgs &a, hipStream_t st)
         return e;
     hipLaunchKernelGGL(kern, dim3(kStreamKGrid), dim3(64 * WAVES), Shape<4>::LDS_BYTES, st, a, tiles_m, tiles_n, p.cut,
                        p.first | p.second << 8);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_tiles(const ExpertLinear &a, hipStream_t st)
+{
+    static_assert(FLEXQ_MAX_EXPERTS < 516, "the offsets' table");
+    const long tiles_n = (a.N + 255) / 256, low = a.group ? 64 : 128;
+    const long bound = (a.slots / low + (a.E < a.slots ? a.E : a.slots)) * tiles_n;
+    if (bound >= (1L << 31)) return hipErrorInvalidValue;
+    const unsigned grid = bound < kStreamKGrid ? (unsigned)((bound + 7) / 8 * 8) : (unsigned)kStreamKGrid;
+    static std::atomic<unsigned long long> allowed[2];
+    const int lds = a.group ? kExpertLds<1> : kExpertLds<0>;
+    const auto kern = a.group ? gemm_expert_kernel<1> : gemm_expert_kernel<0>;
+    if (hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds, allowed[a.group != 0]); e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * WAVES), (size_t)lds, st, a, (int)tiles_n);
     return hipGetLastError();
 }
 

@@ -70,4 +70,47 @@ __device__ __forceinline__ RowGroup find_piece(const int32_t *offsets, int count
     return g;
 }
 
+// Tiles of HIGH rows of a group of n rows, a last one of more than half of that among them (phase 0); the last
+// one where it holds no more than half (phase 1).  offsets: all of them, in order, within the rows.
+template <int HIGH>
+__device__ __forceinline__ int parts_of(int n, int phase)
+{
+    const int rest = n % HIGH;
+    return phase == 0 ? n / HIGH + (rest > HIGH / 2 ? 1 : 0) : (rest > 0 && rest <= HIGH / 2 ? 1 : 0);
+}
+
+template <int HIGH>
+__device__ __forceinline__ int count_parts(const int *offsets, int count, int phase)
+{
+    int mine = 0;
+    for (int e = threadIdx.x & 63; e < count; e += 64) mine += parts_of<HIGH>(max(offsets[e + 1] - offsets[e], 0), phase);
+    return __builtin_amdgcn_readlane(wave_scan(mine), 63);
+}
+
+// Number `index` of those: its group, its first row and the group's end.
+template <int HIGH>
+__device__ __forceinline__ RowGroup find_part(const int *offsets, int count, int phase, int index)
+{
+    const int lane = threadIdx.x & 63;
+    RowGroup g = {0, 0, 1, 0};
+    int before = 0;
+    for (int e0 = 0; e0 < count; e0 += 64) {
+        const int e = min(e0 + lane, count - 1), begin = offsets[e], end = max(offsets[e + 1], begin);
+        const int mine = e0 + lane < count ? parts_of<HIGH>(end - begin, phase) : 0;
+        const int sum = wave_scan(mine), first = before + sum - mine;
+        const unsigned long long hit = __ballot(index >= first && index < first + mine);
+        if (hit) {
+            const int l = __ffsll(hit) - 1;
+            g.id = e0 + l;
+            g.end = __builtin_amdgcn_readlane(end, l);
+            g.tile = index - __builtin_amdgcn_readlane(first, l);
+            const int at = __builtin_amdgcn_readlane(begin, l);
+            g.begin = at + (phase == 0 ? g.tile * HIGH : (g.end - at) / HIGH * HIGH);
+            break;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return g;
+}
+
 }  // namespace

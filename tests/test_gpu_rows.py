@@ -159,7 +159,7 @@ def check_experts(rng, M, E, k, N, K, group, bits, experts, sorted_rows=False, s
     want, slack = ref.expert_rows(codes, sw, xq, sx, order, offsets, 0 if sorted_rows else k, group)
     rows = order[:total] if scatter else np.arange(total)
     rest = np.setdiff1d(np.arange(M * k), rows)
-    for form in range(6):                                     # the library's choice, then every kernel
+    for form in range(7):                                     # the library's choice, then every kernel
         out = torch.full((M * k, N), 7.0, dtype=torch.float16, device=DEV)
         if form == 0:
             fq.expert_linear(*args, out=out, **kw)
