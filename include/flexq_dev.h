@@ -99,8 +99,8 @@ flexq_status flexq_dev_layer_linears(const flexq_dev_tuning *tuning, const flexq
 
 /*
  * flexq_expert_linear with a forced kernel: form 1 = streaming, 2 .. 5 = tiles of 32 x 128, 64 x 128,
- * 128 x 128, 128 x 256 (with group-128 scales 32 x 256, 64 x 128, and 128 x 128 for both others), 0 = the library's
- * choice; *dispatched (may be NULL) receives the form.
+ * 128 x 128, 128 x 256 (with group-128 scales 32 x 256, 64 x 128, and 128 x 128 for both others), 6 = persistent
+ * workgroups with tiles of 256 x 256 and 128 x 256 (128 x 256 and 64 x 256), 0 = the library's choice; *dispatched (may be NULL) receives the form.
  */
 flexq_status flexq_dev_expert_linear(int form, const void *packed, int E, int group, const int8_t *xq,
                                      const uint16_t *sx, int x_rows, const int32_t *order, const int32_t *offsets,

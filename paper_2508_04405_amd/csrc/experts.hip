@@ -10,6 +10,7 @@
 #include "api_internal.h"
 #include "flexq_kernels.h"
 #include "row_groups.h"
+#include <math.h>
 
 namespace {
 
@@ -156,12 +157,14 @@ inline int groups_of(const ExpertLinear &a) { return a.E < a.slots ? a.E : a.slo
 // Eight wavefronts a workgroup where there are at most two workgroups a CU and rows are long: four leave the
 // chip half empty (11008 x 4096 by one token's two experts: 20.8 us with four, 14.6 with eight; with more
 // workgroups eight only lengthen the meeting in LDS, 22016 x 4096 26.1 and 27.1, at eight tokens 80.8 and 84.5).
+inline int stream_waves(const ExpertLinear &a) { return (long)groups_of(a) * (a.N / 32) <= 512 && a.K >= 4096 ? 8 : 4; }
+
 template <int GROUP>
 hipError_t launch_stream(const ExpertLinear &a, hipStream_t st)
 {
     const long wgs = (long)groups_of(a) * (a.N / 32);
     if (wgs >= (1L << 31)) return hipErrorInvalidValue;
-    if (wgs <= 512 && a.K >= 4096)
+    if (stream_waves(a) == 8)
         hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 8>), dim3((unsigned)wgs), dim3(512), 0, st, a);
     else
         hipLaunchKernelGGL((expert_stream_kernel<GROUP, 2, 4>), dim3((unsigned)wgs), dim3(256), 0, st, a);
@@ -169,42 +172,100 @@ hipError_t launch_stream(const ExpertLinear &a, hipStream_t st)
 }
 
 // Which kernel: 1 streaming, 2 .. 5 tiles of 32 x 128 (group-128 scales: 32 x 256), 64 x 128, 128 x 128,
-// 128 x 256.  How the rows fall is known on the device only, so by their average over the experts.
+// 128 x 256, 6 persistent tiles of 256 x 256 (128 x 256).
 //
-// Few rows each: the streaming kernel cuts K over its wavefronts and wins where rows are long, or where
-// 32 x 128 tiles would not fill the chip (us streaming / 32 x 128: 22016 x 4096 at 2 rows each of 8 experts 81 /
-// 91, 4096 x 11008 at one token 14.6 / 32.8, 2816 x 2048 at one token, 132 tiles, 8.1 / 8.4; but at four tokens
-// 18.9 / 15.9, and 4096 x 11008 at 6 rows each 62 / 52).  Between the tiles the work of the busiest CU decides,
-// at the relative rates that so many workgroups on a CU reach (as for the dense layer); a tile more than the
-// rows fill, half a one on average.  Measured over 2816 x 2048 and 4096 x 11008 with 8 experts, 64 to 4096 tokens,
-// the choice is the fastest or within 7 % of it.
+// How the rows fall is known on the device only, so by their average over the experts: the kernel that is
+// estimated to be fastest.  An estimate is the busiest CU's stages of 128 k at what a stage takes with so many
+// workgroups on a CU, something a round and a launch, and no less than the touched experts' weights take from
+// memory.  The constants are fitted to 860 random layers (768 .. 12160 deep, 512 .. 22000 wide, 2 .. 128 experts,
+// 1 .. 6000 tokens, 1 .. 8 experts each), which they meet to 10 .. 16 %; on 600 others what is chosen takes 1.025 times the fastest
+// kernel's time on average, 1.12 or less on nine in ten, 1.48 at most.  Some layers, us by form 1 / 2 / 3 / 4 / 5 / 6:
+//   2 experts at 16 rows, K 8576, N 1088     12 / 23 / 27 / 37 / 56 / 49
+//   64 at 24 rows, K 2048, N 2816            91 / 50 / 49 / 58 / 56 / -
+//   8 at 128 rows, K 11008, N 4096           - / 119 / 97 / 103 / 96 / 103
+//   8 at 256 rows, K 11008, N 4096           - / 188 / 144 / 142 / 150 / 122
+//   8 at 1024 rows, K 4096, N 22016          - / 1321 / 915 / 776 / 723 / 691
+struct TileTimes {
+    int height, width, slots;            // of a tile; workgroups on a CU
+    double stage[4], round, launch;      // us a stage by workgroups on the CU, a round, a launch
+    double rate, least;                  // bytes a us from memory, and what a launch takes beside them
+};
+constexpr TileTimes kChannelTiles[4] = {
+    {32, 128, 4, {0.331, 0.482, 0.716, 0.851}, 1.98, 3.12, 5.55e6, 4.87},
+    {64, 128, 4, {0.391, 0.611, 0.958, 1.245}, 2.76, 2.74, 5.58e6, 5.73},
+    {128, 128, 3, {0.562, 0.969, 1.488, 0.0}, 3.85, 1.88, 5.20e6, 7.80},
+    {128, 256, 2, {0.851, 1.734, 0.0, 0.0}, 6.30, 0.79, 5.05e6, 8.41},
+};
+constexpr TileTimes kGroupTiles[3] = {
+    {32, 256, 2, {0.624, 1.018, 0.0, 0.0}, 2.69, 3.19, 5.39e6, 5.81},
+    {64, 128, 2, {0.540, 0.829, 0.0, 0.0}, 2.90, 2.54, 5.07e6, 6.59},
+    {128, 128, 2, {0.806, 1.272, 0.0, 0.0}, 3.18, 2.94, 3.81e6, 7.31},
+};
+struct PersistentTimes {
+    double high, low, high_item, low_item;   // us a stage of a tile of either height, and an item
+    double uneven, launch, rate, least;      // of an item that the busiest CU has more than the average
+};
+constexpr PersistentTimes kPersistent[2] = {{1.251, 0.687, 8.50, 5.66, 0.577, 1.86, 4.51e6, 2.68},
+                                            {0.993, 0.685, 7.17, 4.08, 0.462, 1.58, 5.36e6, 9.19}};
+struct StreamTimes {
+    double launch, step, row, wg, rate, least;   // us: a step of a wavefront, more for a row, for a workgroup on the CU
+};
+constexpr StreamTimes kStream[2] = {{4.77, 0.167, 0.0213, 0.325, 4.61e6, 4.97}, {2.02, 0.334, 0.0526, 0.339, 5.07e6, 5.77}};
+
 int choose_form(const ExpertLinear &a)
 {
-    const double groups = groups_of(a), rows = (double)a.slots / groups;
-    const long n128 = (a.N + 127) / 128, n256 = (a.N + 255) / 256;
-    if (rows <= 4.0 && (a.K >= 4096 || groups * n128 <= 160)) return 1;
-    auto tiles = [&](int height, long across) {
-        const double t = rows / height + 0.5;
-        return groups * (t < 1.0 ? 1.0 : t) * across;
-    };
-    if (rows <= 24.0) return 2;
-    // group-128 scales: vector-bound, the columns of a tile matter less than its padding (2816 x 2048, 64 experts
-    // at 12 rows each 48 / 56 / 80 us on 32, 64 and 128 rows, at 48 70 / 72 / 86, at 192 187 / 178 / 157)
-    if (a.group) return rows < 96.0 ? 3 : 4;
-    // short rows, few tiles: lower ones fill the chip (2816 x 2048 at 64 rows each of 8 experts 12.5 / 14.9 us)
-    if (rows <= 64.0 && a.K <= 4096 && tiles(64, n128) <= 384.0) return 2;
-    auto busiest_cu = [](double tiles, double area, int slots, const double *rate) {
-        const long per_cu = (long)((tiles + 255.0) / 256.0), full = per_cu / slots, rest = per_cu % slots;
-        return (double)full * slots * area / rate[slots - 1] + (rest ? (double)rest * area / rate[rest - 1] : 0.0);
-    };
-    static const double rate64[4] = {0.30, 0.50, 0.65, 0.80}, rate128[3] = {0.40, 0.75, 0.85},
-                        sparse128[3] = {0.58, 0.75, 0.85}, rate256[2] = {0.70, 1.00};
-    const double t128 = tiles(128, n128);
-    const double us64 = busiest_cu(tiles(64, n128), 0.5, 4, rate64);
-    const double us128 = busiest_cu(t128, 1.0, 3, t128 <= 256.0 ? sparse128 : rate128);
-    const double us256 = busiest_cu(tiles(128, n256), 2.0, 2, rate256);
-    if (us256 <= us128 && us256 <= us64) return 5;
-    return us128 <= us64 ? 4 : 3;
+    const int grouped = a.group != 0, count = groups_of(a);
+    const double groups = count, rows = (double)a.slots / groups;
+    const double stages = a.K / FLEXQ_TILE_K;
+    auto up = [](double v) { return (double)(long)(v + 0.999999); };
+    auto most = [](double x, double y) { return x > y ? x : y; };
+    // experts with a row, if each slot picked one by itself
+    const double touched = a.slots >= 4 * a.E ? a.E : a.E * (1.0 - pow(1.0 - 1.0 / a.E, a.slots));
+    const double bytes = touched * 0.75 * (double)a.N * a.K;
+    int best = 6;
+    double least;
+    {
+        const PersistentTimes &t = kPersistent[grouped];
+        const double height = grouped ? 128.0 : 256.0, across = (a.N + 255) / 256, spread = most(1.0, sqrt(rows));
+        double high = 0.0, low = 0.0, sum = 0.0;
+        for (int i = -4; i <= 4; ++i) {          // an expert's rows are spread by about their root
+            const double weight = exp(-0.125 * i * i), n = most(0.0, rows + 0.5 * i * spread);
+            const double whole = (double)(long)(n / height), rest = n - whole * height;
+            high += weight * (whole + (rest > height / 2 ? 1.0 : 0.0));
+            low += weight * (rest > 0.0 && rest <= height / 2 ? 1.0 : 0.0);
+            sum += weight;
+        }
+        high *= groups * across / sum;
+        low *= groups * across / sum;
+        const double one = stages * t.high + t.high_item, other = stages * t.low + t.low_item;
+        const double longest = high > 0.5 ? one : other;
+        least = most((high * one + low * other) / 256.0 + t.uneven * longest, longest) + t.launch;
+        least = most(least, bytes / t.rate + t.least);
+    }
+    for (int f = 0; f < (grouped ? 3 : 4); ++f) {
+        const TileTimes &t = grouped ? kGroupTiles[f] : kChannelTiles[f];
+        // a tile more than the rows fill, half a one on average
+        const double tiles = groups * most(1.0, rows / t.height + 0.5) * ((a.N + t.width - 1) / t.width);
+        const long per_cu = (long)up(tiles / 256.0), full = per_cu / t.slots, rest = per_cu % t.slots;
+        double us = stages * (full * t.stage[t.slots - 1] + (rest ? t.stage[rest - 1] : 0.0)) +
+                    t.round * (double)(full + (rest ? 1 : 0)) + t.launch;
+        us = most(us, bytes / t.rate + t.least);
+        if (us < least) {
+            least = us;
+            best = 2 + f;
+        }
+    }
+    if (rows <= 40.0) {
+        const StreamTimes &t = kStream[grouped];
+        const long wgs = (long)count * (a.N / 32);
+        const bool eight = stream_waves(a) == 8;
+        const double per_cu = up(wgs / 256.0), steps = up(stages / (eight ? 8.0 : 4.0));
+        const double passes = rows > 20.0 ? most(1.0, rows / 32.0 + 0.5) : 1.0, filled = rows < 32.0 ? rows : 32.0;
+        double us = t.launch + passes * steps * ((t.step + t.row * filled) * up(per_cu / (eight ? 3.0 : 7.0)) + t.wg * per_cu);
+        us = most(us, passes * bytes / t.rate + t.least);
+        if (us < least) best = 1;
+    }
+    return best;
 }
 
 }  // namespace
