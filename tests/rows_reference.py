@@ -44,8 +44,12 @@ def route(logits, k, score, bias=None, groups=1, top_groups=1, group_top=1, reno
                 by = lambda e: c[e]
         chosen = sorted(there, key=lambda e: (-by(e), e))[:k]
         w = s[chosen]
-        if renormalise:
-            w = w / w.sum() if w.sum() > 0 else np.zeros_like(w)
+        if renormalise and chosen:
+            # sigmoids far below 0 are e^l, whose ratios remain where the scores themselves underflow
+            top = l[chosen].max()
+            if top < -700.0:
+                w = np.exp(l[chosen] - top)
+            w = w / w.sum()
         experts[m, :len(chosen)], weights[m, :len(chosen)] = chosen, w * scale
     return experts, weights
 
