@@ -397,6 +397,7 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *   experts  dev, out, int32 [M,k], by falling c        weights  dev, out, fp32 [M,k]
  *   order, offsets  dev, out, or both NULL: the grouping of the M k slots (slot m k + j) over the E experts
  *   workspace       as for flexq_group_rows, flexq_route_workspace_bytes(M, E, k); may be NULL without order
+ *                   and for up to 32 tokens
  * c is made and compared in 64 bits where a bias or a sum enters it, and the logits themselves are
  * compared where none does; weights are good to a few ulp of fp32.
  * 1 <= k <= FLEXQ_MAX_EXPERTS_PER_TOKEN, k <= top_groups * E / groups, groups <= 64, 0 < scale < inf.

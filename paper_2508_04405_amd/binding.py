@@ -434,14 +434,27 @@ def layer_linears(layer, M, workspace, first_stage=0, last_stage=3, **buffers):
 
 Routing = collections.namedtuple("Routing", "experts weights order offsets")
 _SCORES = {"softmax": 0, "sigmoid": 1}
+_ROUTE_ONE_LAUNCH = 32                  # tokens that flexq_route groups without a workspace
 
 
-def _here(t, dtype, *shape):
-    """A contiguous tensor of this type and shape on the current device (whose stream the call uses)."""
-    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
+def _current(t):
+    """The current device (whose stream the call uses), which the call's first tensor must be on."""
+    d = t.get_device()
+    if d < 0 or d != torch._C._cuda_getDevice():
         raise FlexQError(f"flexq: a tensor is on {t.device}, the call runs on the current device")
-    if t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise FlexQError(f"flexq: expected a contiguous {dtype} tensor of {list(shape)}, got {t.dtype} {list(t.shape)}")
+    return d
+
+
+def _refuse(t, dtype, shape):
+    raise FlexQError(f"flexq: expected a contiguous {dtype} tensor of {list(shape)} on the current device, got {t.dtype} "
+                     f"{list(t.shape)} on {t.device}")
+
+
+def _here(t, dtype, shape, dev):
+    """A contiguous tensor of this type and shape on device `dev`.  (Small calls are bound by what Python does before
+    them: a check is 0.3 us this way, 0.8 by torch.device objects.)"""
+    if t.get_device() != dev or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(t, dtype, shape)
     return t
 
 
@@ -455,12 +468,13 @@ def group_rows(ids, count, workspace=None):
     """int32 ids (any shape; outside 0 .. count - 1: no group) -> (order, offsets): the rows by group, each
     group's in ascending order, those without one last, and where each group begins."""
     lib = load()
-    _here(ids, torch.int32, *ids.shape)
-    rows = ids.numel()
-    ws = _scratch(lib.flexq_group_rows_workspace_bytes(rows, count), workspace, ids.device)
-    order = torch.empty(rows, dtype=torch.int32, device=ids.device)
-    offsets = torch.empty(count + 1, dtype=torch.int32, device=ids.device)
-    _check(lib.flexq_group_rows(_ptr(ids), rows, count, _ptr(order), _ptr(offsets), _ptr(ws), ws.numel(), _stream()))
+    _here(ids, torch.int32, ids.shape, _current(ids))
+    rows, dev = ids.numel(), ids.device
+    ws = _scratch(lib.flexq_group_rows_workspace_bytes(rows, count), workspace, dev)
+    order = torch.empty(rows, dtype=torch.int32, device=dev)
+    offsets = torch.empty(count + 1, dtype=torch.int32, device=dev)
+    _check(lib.flexq_group_rows(ids.data_ptr(), rows, count, order.data_ptr(), offsets.data_ptr(), ws.data_ptr(), ws.numel(),
+                                _stream()))
     return order, offsets
 
 
@@ -469,23 +483,31 @@ def route_experts(logits, k, score="softmax", bias=None, groups=1, top_groups=1,
     """Scores of the experts, fp32 or fp16 [M,E] -> Routing(experts int32 [M,k], weights fp32 [M,k], and with
     `group` the grouping (order, offsets) of the M * k slots by expert, else None)."""
     lib = load()
-    if score not in _SCORES:
+    kind = _SCORES.get(score)
+    if kind is None:
         raise FlexQError(f"flexq: score is one of {sorted(_SCORES)}, got {score!r}")
-    if logits.dtype not in (torch.float32, torch.float16) or logits.dim() != 2:
-        raise FlexQError(f"flexq: logits are fp32 or fp16 [M, E], got {logits.dtype} {list(logits.shape)}")
+    dtype = logits.dtype
+    if (dtype != torch.float32 and dtype != torch.float16) or logits.dim() != 2:
+        raise FlexQError(f"flexq: logits are fp32 or fp16 [M, E], got {dtype} {list(logits.shape)}")
     M, E = logits.shape
-    _here(logits, logits.dtype, M, E)
+    cur = _current(logits)
+    _here(logits, dtype, (M, E), cur)
     if bias is not None:
-        _here(bias, torch.float32, E)
+        _here(bias, torch.float32, (E,), cur)
     dev = logits.device
-    r = _Routing(k, _SCORES[score], groups, top_groups, group_top, int(bool(renormalise)), float(scale), _ptr(bias))
-    ws = _scratch(lib.flexq_route_workspace_bytes(M, E, k), workspace, dev) if group else None
+    r = _Routing(k, kind, groups, top_groups, group_top, 1 if renormalise else 0, scale, None if bias is None else bias.data_ptr())
+    nbytes = lib.flexq_route_workspace_bytes(M, E, k)
+    if nbytes == 0:
+        raise FlexQError("flexq: invalid number of tokens, experts or experts a token")
     experts = torch.empty((M, k), dtype=torch.int32, device=dev)
     weights = torch.empty((M, k), dtype=torch.float32, device=dev)
-    order = torch.empty(M * k, dtype=torch.int32, device=dev) if group else None
-    offsets = torch.empty(E + 1, dtype=torch.int32, device=dev) if group else None
-    _check(lib.flexq_route(_ptr(logits), int(logits.dtype == torch.float16), M, E, ctypes.byref(r), _ptr(experts),
-                           _ptr(weights), _ptr(order), _ptr(offsets), _ptr(ws), ws.numel() if group else 0, _stream()))
+    order = offsets = ws = None
+    if group:
+        ws = workspace if workspace is not None or M <= _ROUTE_ONE_LAUNCH else torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        order = torch.empty(M * k, dtype=torch.int32, device=dev)
+        offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
+    _check(lib.flexq_route(logits.data_ptr(), 1 if dtype == torch.float16 else 0, M, E, ctypes.byref(r), experts.data_ptr(),
+                           weights.data_ptr(), _ptr(order), _ptr(offsets), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
     return Routing(experts, weights, order, offsets)
 
 
@@ -506,15 +528,15 @@ def expert_linear(packed, N, K, xq, sx, order, offsets, group=0, k=0, scatter=Fa
     nbytes = lib.flexq_packed_bytes(N, K, group)
     if nbytes == 0:
         raise FlexQError("flexq: invalid shape or group of the experts' weights")
-    E, slots, rows = packed.shape[0], order.numel(), xq.shape[0]
-    _here(packed, torch.uint8, E, nbytes)
-    _here(xq, torch.int8, rows, K)
-    _here(sx, torch.float16, rows)
-    _here(order, torch.int32, slots)
-    _here(offsets, torch.int32, E + 1)
-    y = torch.empty((slots, N), dtype=torch.float16, device=xq.device) if out is None else _here(out, torch.float16, slots, N)
-    _check(lib.flexq_expert_linear(_ptr(packed), E, group, _ptr(xq), _ptr(sx), rows, _ptr(order), _ptr(offsets), slots, k,
-                                   int(bool(scatter)), N, K, _ptr(y), _stream()))
+    E, slots, rows, cur = packed.shape[0], order.numel(), xq.shape[0], _current(xq)
+    _here(packed, torch.uint8, (E, nbytes), cur)
+    _here(xq, torch.int8, (rows, K), cur)
+    _here(sx, torch.float16, (rows,), cur)
+    _here(order, torch.int32, (slots,), cur)
+    _here(offsets, torch.int32, (E + 1,), cur)
+    y = torch.empty((slots, N), dtype=torch.float16, device=xq.device) if out is None else _here(out, torch.float16, (slots, N), cur)
+    _check(lib.flexq_expert_linear(packed.data_ptr(), E, group, xq.data_ptr(), sx.data_ptr(), rows, order.data_ptr(),
+                                   offsets.data_ptr(), slots, k, 1 if scatter else 0, N, K, y.data_ptr(), _stream()))
     return y
 
 
@@ -523,14 +545,15 @@ def combine_experts(y, experts, weights, add=None, out=None):
     plus fp16 add [M,N] if given -> fp16 [M,N].  Slots with a negative expert are left out."""
     lib = load()
     M, k = experts.shape
-    N = y.shape[1]
-    _here(y, torch.float16, M * k, N)
-    _here(experts, torch.int32, M, k)
-    _here(weights, torch.float32, M, k)
+    N, cur = y.shape[1], _current(y)
+    _here(y, torch.float16, (M * k, N), cur)
+    _here(experts, torch.int32, (M, k), cur)
+    _here(weights, torch.float32, (M, k), cur)
     if add is not None:
-        _here(add, torch.float16, M, N)
-    res = torch.empty((M, N), dtype=torch.float16, device=y.device) if out is None else _here(out, torch.float16, M, N)
-    _check(lib.flexq_expert_combine(_ptr(y), _ptr(experts), _ptr(weights), _ptr(add), M, k, N, _ptr(res), _stream()))
+        _here(add, torch.float16, (M, N), cur)
+    res = torch.empty((M, N), dtype=torch.float16, device=y.device) if out is None else _here(out, torch.float16, (M, N), cur)
+    _check(lib.flexq_expert_combine(y.data_ptr(), experts.data_ptr(), weights.data_ptr(), _ptr(add), M, k, N, res.data_ptr(),
+                                    _stream()))
     return res
 
 
@@ -541,15 +564,16 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
     lib = load()
     L, R, K = a.shape
     M, N = y.shape
-    _here(a, torch.float16, L, R, K)
-    _here(b, torch.float16, L, N, R)
-    _here(scale, torch.float32, L)
-    _here(x, torch.float16, M, K)
-    _here(y, torch.float16, M, N)
-    _here(order, torch.int32, M)
-    _here(offsets, torch.int32, L + 1)
+    cur, half, i32 = _current(x), torch.float16, torch.int32
+    _here(a, half, (L, R, K), cur)
+    _here(b, half, (L, N, R), cur)
+    _here(scale, torch.float32, (L,), cur)
+    _here(x, half, (M, K), cur)
+    _here(y, half, (M, N), cur)
+    _here(order, i32, (M,), cur)
+    _here(offsets, i32, (L + 1,), cur)
     ws = _scratch(lib.flexq_adapters_workspace_bytes(M, L, R, K), workspace, x.device)
-    res = torch.empty((M, N), dtype=torch.float16, device=x.device) if out is None else _here(out, torch.float16, M, N)
-    _check(lib.flexq_adapters(_ptr(a), _ptr(b), _ptr(scale), L, R, _ptr(x), _ptr(order), _ptr(offsets), M, N, K, _ptr(y),
-                              _ptr(res), _ptr(ws), ws.numel(), _stream()))
+    res = torch.empty((M, N), dtype=half, device=x.device) if out is None else _here(out, half, (M, N), cur)
+    _check(lib.flexq_adapters(a.data_ptr(), b.data_ptr(), scale.data_ptr(), L, R, x.data_ptr(), order.data_ptr(),
+                              offsets.data_ptr(), M, N, K, y.data_ptr(), res.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return res

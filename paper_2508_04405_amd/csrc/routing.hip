@@ -623,8 +623,8 @@ flexq_status flexq_route(const void *logits, int half, int M, int E, const flexq
     static_assert(2 * kWaves * FLEXQ_MAX_EXPERTS_PER_TOKEN <= kOneBlock, "a block's slots");
     const bool one = M <= 2 * kWaves;
     if (order) {
-        if (!workspace || workspace_bytes < hist_bytes(M, R->k, E)) return FLEXQ_EWORKSPACE;
-        if (!aligned16(workspace)) return FLEXQ_EALIGN;
+        if (!one && (!workspace || workspace_bytes < hist_bytes(M, R->k, E))) return FLEXQ_EWORKSPACE;
+        if (!one && !aligned16(workspace)) return FLEXQ_EALIGN;
         if (one) {
             a.per_block = M;
             a.order = order;

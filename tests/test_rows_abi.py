@@ -64,6 +64,7 @@ def test_route_refusals():
         assert call(**kw) == EALIGN, kw
     assert call(dict(bias=0x1002)) == EALIGN
     assert call(ws=None) == EWORKSPACE and call(wsb=16) == EWORKSPACE
+    assert call(M=33, ws=None) == EWORKSPACE                               # from there on two launches
 
 
 def test_expert_linear_refusals():
