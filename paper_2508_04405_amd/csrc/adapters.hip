@@ -21,7 +21,6 @@
 namespace {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-constexpr int kRows = 16;                // rows of a piece
 constexpr int kMaxRank = FLEXQ_MAX_RANK;
 
 struct AdapterArgs {
@@ -39,40 +38,74 @@ __device__ __forceinline__ v4f mfma_h(v8h a, v8h b, v4f c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// RT: tiles of 16 ranks that a workgroup makes; grid: pieces x rank chunks x K splits.
-template <int RT>
+// RT: tiles of 16 ranks that a workgroup makes; RB: rows of a piece, by 16; grid: pieces x rank chunks x K splits.
+// A step is 64 k, a line of every row of x; U steps' loads set out together.
+// EXACT: R is a multiple of RT tiles.
+template <int RT, int RB, int U, bool EXACT>
 __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs p, int chunks)
 {
-    __shared__ float red[4][RT * 16][kRows + 1];
+    constexpr int ROWS = 16 * RB;
+    __shared__ float red[4][RT * 16][ROWS + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int id = blockIdx.x;
     const int split = id % p.splits;
     id /= p.splits;
     const int r0 = id % chunks * RT * 16;
-    const RowGroup g = find_piece(p.offsets, p.L, p.M, kRows, id / chunks);
+    const RowGroup g = find_piece(p.offsets, p.L, p.M, ROWS, id / chunks);
     if (g.id < 0) return;
-    const int first = g.begin + kRows * g.tile, rows = min(kRows, g.end - first);
-    const int row = min(max(p.order[first + min(lane & 15, rows - 1)], 0), p.M - 1);
-    const int steps = p.K / 32;
+    const int first = g.begin + ROWS * g.tile, rows = min(ROWS, g.end - first);
+    const int steps = p.K / 64;
     const int s0 = (int)((long)split * steps / p.splits), s1 = (int)((long)(split + 1) * steps / p.splits);
-    const uint16_t *x = p.x + (size_t)row * p.K + 8 * (lane >> 4);
+    const uint16_t *x[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int row = min(max(p.order[first + min(16 * b + (lane & 15), rows - 1)], 0), p.M - 1);
+        x[b] = p.x + (size_t)row * p.K + 8 * (lane >> 4);
+    }
     const uint16_t *a = p.a + ((size_t)g.id * p.R + r0 + (lane & 15)) * p.K + 8 * (lane >> 4);
-    const int live = min(RT, (p.R - r0) / 16);
-    v4f acc[RT];
+    const int live = EXACT ? RT : min(RT, (p.R - r0) / 16);
+    v4f acc[RT][RB];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] = 0.0f;
-    for (int s = s0 + wave; s < s1; s += 4) {
-        const v8h xv = *reinterpret_cast<const v8h *>(x + 32 * (size_t)s);
+        for (int b = 0; b < RB; ++b) acc[t][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = s0 + wave; s < s1; s += 4 * U) {
+        v8h xv[U][RB][2], av[U][RT][2];
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-            if (t < live) acc[t] = mfma_h(*reinterpret_cast<const v8h *>(a + (size_t)16 * t * p.K + 32 * (size_t)s), xv, acc[t]);
+        for (int u = 0; u < U; ++u)
+            if (s + 4 * u < s1) {
+                const size_t k = (size_t)64 * (s + 4 * u);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) xv[u][b][h] = *reinterpret_cast<const v8h *>(x[b] + k + 32 * h);
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+                    if (t < live) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            av[u][t][h] = *reinterpret_cast<const v8h *>(a + (size_t)16 * t * p.K + k + 32 * h);
+                    }
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (s + 4 * u < s1) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+                    if (t < live) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int b = 0; b < RB; ++b) acc[t][b] = mfma_h(av[u][t][h], xv[u][b][h], acc[t][b]);
+                    }
+            }
     }
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) red[wave][16 * t + 4 * (lane >> 4) + i][lane & 15] = acc[t][i];
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][16 * t + 4 * (lane >> 4) + i][16 * b + (lane & 15)] = acc[t][b][i];
     __syncthreads();
     for (int i = tid; i < live * 16 * rows; i += 256) {
         const int m = i / (live * 16), r = i % (live * 16);
@@ -80,113 +113,201 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(AdapterArgs p, int ch
     }
 }
 
-// RT: tiles of 16 ranks, the last ones may be empty.
-template <int RT>
+// Ranks by 32, of which the kernel is laid out for up to F, hi and lo in an MFMA each; 16 that are left over, hi
+// and lo, in one.  RB: rows of a piece, by 16.  EXACT: R is 32 F, or 16.
+template <int F, int RB, bool EXACT>
 __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs p, int rest)
 {
-    __shared__ __attribute__((aligned(16))) _Float16 h[kRows][RT * 32 + 8];   // hi 16, lo 16 ranks by turns
-    __shared__ float back[kRows];                                             // what undoes a row's power of two, times scale
+    constexpr int ROWS = 16 * RB;
+    constexpr int RT = EXACT && F > 0 ? 2 * F : 2 * F + 1;   // tiles of 16 ranks
+    constexpr int STRIDE = RT * 16 + 8;                      // (padded against bank conflicts)
+    __shared__ __attribute__((aligned(16))) _Float16 h[2][ROWS][STRIDE];      // hi, lo
+    __shared__ float back[ROWS];                             // what undoes a row's power of two, times scale
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int column_blocks = (p.N + p.columns - 1) / p.columns;
     const int c0 = blockIdx.x % column_blocks * p.columns, c1 = min(p.N, c0 + p.columns);
-    const RowGroup g = find_piece(p.offsets, p.L, p.M, kRows, blockIdx.x / column_blocks, rest != 0);
+    const RowGroup g = find_piece(p.offsets, p.L, p.M, ROWS, blockIdx.x / column_blocks, rest != 0);
     if (g.id < 0) return;
-    const int first = g.begin + kRows * g.tile, rows = min(kRows, g.end - first);
-    const int row = min(max(p.order[first + min(lane & 15, rows - 1)], 0), p.M - 1);
-    const bool mine = (lane & 15) < rows;
+    const int first = g.begin + ROWS * g.tile, rows = min(ROWS, g.end - first);
+    size_t at[RB];                                           // this lane's rows' first columns in y and out
+    bool mine[RB];
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+        const int m = 16 * k + (lane & 15);
+        mine[k] = m < rows;
+        const int row = min(max(p.order[first + min(m, rows - 1)], 0), p.M - 1);
+        at[k] = (size_t)row * p.N + 16 * (lane >> 4);
+    }
+    auto load_y = [&](uint4 (&v)[2], int k, int n0) {
+        if (mine[k] && n0 + 16 * (lane >> 4) < c1) {
+            v[0] = reinterpret_cast<const uint4 *>(p.y + at[k] + n0)[0];
+            v[1] = reinterpret_cast<const uint4 *>(p.y + at[k] + n0)[1];
+        }
+    };
+    auto store = [&](const uint4 (&v)[2], int k, int n0) {
+        if (mine[k] && n0 + 16 * (lane >> 4) < c1) {
+            reinterpret_cast<uint4 *>(p.out + at[k] + n0)[0] = v[0];
+            reinterpret_cast<uint4 *>(p.out + at[k] + n0)[1] = v[1];
+        }
+    };
     if (g.id == p.L) {                   // rows without an adapter
-        for (int n = c0 + 64 * wave + 16 * (lane >> 4); n < c1; n += 256)
-            if (mine) {
-                const uint4 *from = reinterpret_cast<const uint4 *>(p.y + (size_t)row * p.N + n);
-                uint4 *to = reinterpret_cast<uint4 *>(p.out + (size_t)row * p.N + n);
-                const uint4 u = from[0], v = from[1];
-                to[0] = u;
-                to[1] = v;
+        for (int n0 = c0 + 64 * wave; n0 < c1; n0 += 256)
+#pragma unroll
+            for (int k = 0; k < RB; ++k) {
+                uint4 v[2] = {};
+                load_y(v, k, n0);
+                store(v, k, n0);
             }
         return;
     }
-    const int live = p.R / 16;
-    {
-        const int m = tid >> 4, q = tid & 15;
-        float v[RT], top = 0.0f;
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            v[t] = 0.0f;
-            if (t < live && m < rows)
-                for (int s = 0; s < p.splits; ++s) v[t] += p.h[((size_t)s * p.M + first + m) * p.R + 16 * t + q];
-            top = fmaxf(top, fabsf(v[t]));
-        }
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-        int e = 0;
-        if (top > 0.0f) e = 14 - (__builtin_amdgcn_frexp_expf(top));
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const float w = __builtin_amdgcn_ldexpf(v[t], e);
-            const _Float16 hi = (_Float16)w;
-            h[m][32 * t + q] = hi;
-            h[m][32 * t + 16 + q] = (_Float16)(w - (float)hi);
-        }
-        if (q == 0) back[m] = __builtin_amdgcn_ldexpf(p.scale[g.id], -e);
-    }
-    __syncthreads();
-    v8h hv[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) hv[t] = *reinterpret_cast<const v8h *>(&h[lane & 15][32 * t + 8 * (lane >> 4)]);
-    const float undo = back[lane & 15];
+    const int full = EXACT ? F : p.R / 32, tail = EXACT ? F == 0 : p.R / 16 & 1, live = EXACT ? RT : p.R / 16;
     // MFMA row i of tile t is column 16 (i / 4) + 4 t + i % 4 of 64: a lane's results are 16 in a row
     const int i = lane & 15;
-    const uint16_t *b = p.b + (size_t)g.id * p.N * p.R + 8 * ((lane >> 4) & 1);
-    for (int n0 = c0 + 64 * wave; n0 < c1; n0 += 256) {
-        v4f acc[4];
+    const uint16_t *b = p.b + (size_t)g.id * p.N * p.R;
+    struct Stage {
+        v8h full[4][F > 0 ? F : 1], tail[4];
+        uint4 y[RB][2];
+    };
+    auto load = [&](Stage &s, int n0) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int n = min(n0 + 16 * (i >> 2) + 4 * t + (i & 3), p.N - 1);
-            acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            const uint16_t *from = b + (size_t)min(n0 + 16 * (i >> 2) + 4 * t + (i & 3), p.N - 1) * p.R;
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-                if (r < live) acc[t] = mfma_h(*reinterpret_cast<const v8h *>(b + (size_t)n * p.R + 16 * r), hv[r], acc[t]);
+            for (int f = 0; f < F; ++f)
+                if (f < full) s.full[t][f] = *reinterpret_cast<const v8h *>(from + 32 * f + 8 * (lane >> 4));
+            if (tail) s.tail[t] = *reinterpret_cast<const v8h *>(from + 32 * full + 8 * ((lane >> 4) & 1));
         }
-        const int n = n0 + 16 * (lane >> 4);
-        if (mine && n < c1) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(p.y + (size_t)row * p.N + n);
-            uint4 *to = reinterpret_cast<uint4 *>(p.out + (size_t)row * p.N + n);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint4 v = from[u];
-                const unsigned w[4] = {v.x, v.y, v.z, v.w};
-                unsigned o[4];
+        for (int k = 0; k < RB; ++k) load_y(s.y[k], k, n0);
+    };
+    Stage st;                            // the first columns' operands set out ahead of h
+    int n0 = c0 + 64 * wave;
+    if (n0 < c1) load(st, n0);
+    {
+        const int q = tid & 15;
+        float v[RB][RT];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float lo = __builtin_fmaf(acc[2 * u + j / 2][2 * (j & 1)], undo, h2f((uint16_t)w[j]));
-                    const float hi = __builtin_fmaf(acc[2 * u + j / 2][2 * (j & 1) + 1], undo, h2f((uint16_t)(w[j] >> 16)));
-                    o[j] = (unsigned)f2h(lo) | ((unsigned)f2h(hi) << 16);
-                }
-                to[u] = make_uint4(o[0], o[1], o[2], o[3]);
+        for (int k = 0; k < RB; ++k)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) v[k][t] = 0.0f;
+        // (all of a split's shares set out together: one after the other they are most of a small call)
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+            for (int k = 0; k < RB; ++k) {
+                const int m = min(16 * k + (tid >> 4), rows - 1);     // (rows beyond the last repeat it and are not stored)
+                const float *from = p.h + ((size_t)s * p.M + first + m) * p.R + q;
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+                    if (t < live) v[k][t] += from[16 * t];
             }
+#pragma unroll
+        for (int k = 0; k < RB; ++k) {
+            const int m = 16 * k + (tid >> 4);
+            float top = 0.0f;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) top = fmaxf(top, fabsf(v[k][t]));
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+            int e = 0;
+            if (top > 0.0f) e = 14 - (__builtin_amdgcn_frexp_expf(top));
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const float w = __builtin_amdgcn_ldexpf(v[k][t], e);
+                const _Float16 hi = (_Float16)w;
+                h[0][m][16 * t + q] = hi;
+                h[1][m][16 * t + q] = (_Float16)(w - (float)hi);
+            }
+            if (q == 0) back[m] = __builtin_amdgcn_ldexpf(p.scale[g.id], -e);
         }
+    }
+    __syncthreads();
+    v8h hi[RB][F > 0 ? F : 1], lo[RB][F > 0 ? F : 1], both[RB];
+    float undo[RB];
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            hi[k][f] = *reinterpret_cast<const v8h *>(&h[0][16 * k + i][32 * f + 8 * (lane >> 4)]);
+            lo[k][f] = *reinterpret_cast<const v8h *>(&h[1][16 * k + i][32 * f + 8 * (lane >> 4)]);
+        }
+        both[k] = *reinterpret_cast<const v8h *>(&h[lane >> 5][16 * k + i][(tail ? 32 * full : 0) + 8 * ((lane >> 4) & 1)]);
+        undo[k] = back[16 * k + i];
+    }
+    for (; n0 < c1; n0 += 256) {
+        v4f acc[RB][4];
+#pragma unroll
+        for (int k = 0; k < RB; ++k)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                acc[k][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int f = 0; f < F; ++f)
+                    if (f < full) {
+                        acc[k][t] = mfma_h(st.full[t][f], hi[k][f], acc[k][t]);
+                        acc[k][t] = mfma_h(st.full[t][f], lo[k][f], acc[k][t]);
+                    }
+                if (tail) acc[k][t] = mfma_h(st.tail[t], both[k], acc[k][t]);
+            }
+        uint4 v[RB][2];
+#pragma unroll
+        for (int k = 0; k < RB; ++k) {
+            const unsigned w[8] = {st.y[k][0].x, st.y[k][0].y, st.y[k][0].z, st.y[k][0].w,
+                                   st.y[k][1].x, st.y[k][1].y, st.y[k][1].z, st.y[k][1].w};
+            unsigned o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float even = __builtin_fmaf(acc[k][j / 2][2 * (j & 1)], undo[k], h2f((uint16_t)w[j]));
+                const float odd = __builtin_fmaf(acc[k][j / 2][2 * (j & 1) + 1], undo[k], h2f((uint16_t)(w[j] >> 16)));
+                o[j] = (unsigned)f2h(even) | ((unsigned)f2h(odd) << 16);
+            }
+            v[k][0] = make_uint4(o[0], o[1], o[2], o[3]);
+            v[k][1] = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+        if (n0 + 256 < c1) load(st, n0 + 256);
+#pragma unroll
+        for (int k = 0; k < RB; ++k) store(v[k], k, n0);
     }
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Pieces of 16 rows that M rows of L adapters can come in.
-long pieces_bound(int M, int L) { return (M + kRows - 1) / kRows + (L < M ? L : M); }
+// Rows of a piece, by 16: two where an adapter has 24 rows or more on average -- A and B, from L2, then feed twice
+// the rows.
+int row_blocks(int M, int L, int R) { return R <= 128 && M >= 24 * (long)(L < M ? L : M) ? 2 : 1; }
 
-// K splits of the first launch: until there are about two workgroups a CU, but 512 k (four steps a
+// Pieces that M rows of `groups` groups can come in, and about how many they will be.
+long pieces_bound(int M, int groups, int height) { return M / height + (groups < M ? groups : M); }
+long pieces_likely(int M, int groups, int height) { return (M + height - 1) / height + (groups < M ? groups : M) / 2; }
+
+// K splits of the first launch: until there are about two workgroups a CU, but 512 k (two steps a
 // wavefront) or more each.
-int splits_for(int M, int L, int K)
+int splits_for(int M, int L, int R, int K)
 {
-    const long pieces = (M + kRows - 1) / kRows + (L < M ? L : M) / 2;
-    long s = 512 / pieces;
-    if (s > K / 512) s = K / 512;
+    const long pieces = pieces_likely(M, L, 16 * row_blocks(M, L, R));
+    long s = (512 + pieces - 1) / pieces;
+    const int least = pieces <= 8 ? 512 : 1024;
+    if (s > K / least) s = K / least;
     return s < 1 ? 1 : s > 64 ? 64 : (int)s;
+}
+
+// Columns of a workgroup of the second launch, 256 a step: one step where that gives few workgroups, else 2, 4 ..
+// until they are about as many as the chip takes well.  Low ranks are bound by memory and want many in flight
+// (us by 1 / 2 / 4 / 8 steps: rank 16 of 4096 x 12288 71 / 64 / 62 / 70, of 4096 x 4096 33 / 31 / 33 / 34); with
+// higher ones two workgroups fill a CU's registers and each begins dearer, with its rows, h and first operands
+// (rank 64 of 2048 x 8192 81 / 60 / 51 / 51, of 48 x 10240 18.5 / 17.8 / 18.7 / 23.8, 128 of 1024 x 4096 32 / 32 / 38 / 48).
+int up_columns(long pieces, int N, int tiles, int blocks)
+{
+    const long most = tiles <= 2 ? 2100 : blocks == 2 ? 768 : 1024;
+    int steps = 1;
+    while (steps < 16 && pieces * ((N + 256 * steps - 1) / (256 * steps)) > most) steps *= 2;
+    return 256 * steps;
 }
 
 size_t workspace_bytes_for(int M, int L, int R, int K)
 {
-    return ((size_t)splits_for(M, L, K) * M * R * 4 + 255) / 256 * 256;
+    return ((size_t)splits_for(M, L, R, K) * M * R * 4 + 255) / 256 * 256;
 }
 
 bool shape_ok(int L, int R, int M, int K)
@@ -232,34 +353,52 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
     p.M = M;
     p.N = N;
     p.K = K;
-    p.splits = splits_for(M, L, K);
-    const long pieces = pieces_bound(M, L);
-    p.columns = 256;
-    while (p.columns < 2048 && pieces * (N / (2 * p.columns)) >= 1024) p.columns *= 2;
-    hipStream_t st = (hipStream_t)stream;
-    const int tiles = R / 16;
-    auto down = [&](auto kern, int rt) {
-        const int chunks = (tiles + rt - 1) / rt;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(pieces * chunks * p.splits)), dim3(256), 0, st, p, chunks);
-        return hipGetLastError();
-    };
-    hipError_t e = tiles == 1   ? down(adapter_down_kernel<1>, 1)
-                   : tiles == 2 ? down(adapter_down_kernel<2>, 2)
-                   : tiles <= 4 ? down(adapter_down_kernel<4>, 4)
-                                : down(adapter_down_kernel<8>, 8);
-    if (e != hipSuccess) return FLEXQ_EHIP;
+    p.splits = splits_for(M, L, R, K);
+    const int blocks = row_blocks(M, L, R), height = 16 * blocks, tiles = R / 16;
     // the rows without an adapter need no products, and nothing at all where out is y
     const int rest = out != y ? 1 : 0;
-    const unsigned blocks = (unsigned)(pieces_bound(M, L + rest) * ((N + p.columns - 1) / p.columns));
-    auto up = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, st, p, rest);
+    p.columns = up_columns(pieces_likely(M, L + rest, height), N, tiles, blocks);
+    hipStream_t st = (hipStream_t)stream;
+    const int rt = tiles == 1 ? 1 : tiles == 2 ? 2 : 4, chunks = (tiles + rt - 1) / rt;
+    const unsigned down_grid = (unsigned)(pieces_bound(M, L, height) * chunks * p.splits);
+    const unsigned up_grid = (unsigned)(pieces_bound(M, L + rest, height) * ((N + p.columns - 1) / p.columns));
+    auto down = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(down_grid), dim3(256), 0, st, p, chunks);
         return hipGetLastError();
     };
-    e = tiles == 1   ? up(adapter_up_kernel<1>)
-        : tiles == 2 ? up(adapter_up_kernel<2>)
-        : tiles <= 4 ? up(adapter_up_kernel<4>)
-        : tiles <= 8 ? up(adapter_up_kernel<8>)
-                     : up(adapter_up_kernel<16>);
+    auto up = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(up_grid), dim3(256), 0, st, p, rest);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (blocks == 2)
+        e = rt == 1          ? down(adapter_down_kernel<1, 2, 4, true>)
+            : rt == 2        ? down(adapter_down_kernel<2, 2, 2, true>)
+            : tiles % 4 == 0 ? down(adapter_down_kernel<4, 2, 2, true>)
+                             : down(adapter_down_kernel<4, 2, 2, false>);
+    else
+        e = rt == 1          ? down(adapter_down_kernel<1, 1, 4, true>)
+            : rt == 2        ? down(adapter_down_kernel<2, 1, 4, true>)
+            : tiles % 4 == 0 ? down(adapter_down_kernel<4, 1, 2, true>)
+                             : down(adapter_down_kernel<4, 1, 2, false>);
+    if (e != hipSuccess) return FLEXQ_EHIP;
+    if (blocks == 2)
+        switch (tiles) {
+        case 1: e = up(adapter_up_kernel<0, 2, true>); break;
+        case 2: e = up(adapter_up_kernel<1, 2, true>); break;
+        case 4: e = up(adapter_up_kernel<2, 2, true>); break;
+        case 8: e = up(adapter_up_kernel<4, 2, true>); break;
+        default: e = up(adapter_up_kernel<3, 2, false>);
+        }
+    else
+        switch (tiles) {
+        case 1: e = up(adapter_up_kernel<0, 1, true>); break;
+        case 2: e = up(adapter_up_kernel<1, 1, true>); break;
+        case 4: e = up(adapter_up_kernel<2, 1, true>); break;
+        case 8: e = up(adapter_up_kernel<4, 1, true>); break;
+        case 16: e = up(adapter_up_kernel<8, 1, true>); break;
+        default: e = tiles < 8 ? up(adapter_up_kernel<3, 1, false>) : up(adapter_up_kernel<7, 1, false>);
+        }
     return e == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
 }
 
