@@ -153,11 +153,14 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs p, int rest
     if (g.id == p.L) {                   // rows without an adapter
         for (int n0 = c0 + 64 * wave; n0 < c1; n0 += 256)
 #pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                uint4 v[2] = {};
-                load_y(v, k, n0);
-                store(v, k, n0);
-            }
+            for (int k = 0; k < RB; ++k)
+                if (mine[k] && n0 + 16 * (lane >> 4) < c1) {
+                    const uint4 *from = reinterpret_cast<const uint4 *>(p.y + at[k] + n0);
+                    uint4 *to = reinterpret_cast<uint4 *>(p.out + at[k] + n0);
+                    const uint4 u = from[0], v = from[1];
+                    to[0] = u;
+                    to[1] = v;
+                }
         return;
     }
     const int full = EXACT ? F : p.R / 32, tail = EXACT ? F == 0 : p.R / 16 & 1, live = EXACT ? RT : p.R / 16;
