@@ -6,14 +6,16 @@
 // > 1) among groups by the sum of a group's best one or two c, then among the experts of the kept
 // groups; the weights are the chosen s.  Two experts whose c are close must not change places with
 // the rounding of an exponential.  Where nothing is added to a score, s grows with l, and l itself,
-// exact, is compared (no exponential but the chosen ones').  Else c is made in fp32, good to 2^-20 of
-// its size (at least 1), and whoever comes next to a chosen one closer than twice that sends the
-// token through the same steps again in 64 bits -- one token in some hundreds.
+// exact, is compared (no exponential but the chosen ones').  Else c is made in fp32, good to 2^-21 of
+// its size (at least 1), and where two that follow each other come closer than twice that, they are
+// made again in 64 bits: of sigmoids the chosen and whoever is that close behind them alone, a lane
+// each (one token in a thousand); all, through the same steps, where that does not suffice.
 //
-// One wavefront a token, expert e in lane e / V: a tie is won by the lowest index.  Values are
-// compared as unsigned keys (the bits of a float or double, so mapped that they order like the
-// values, and 0 for what cannot be chosen): a round is the DPP maximum over the lanes, its place by
-// ballots, on the scalar unit.
+// Sixteen lanes a token, four tokens a wavefront, expert e in lane e / V: a tie is won by the lowest
+// index.  Values are compared as unsigned keys (the bits of a float or double, so mapped that they
+// order like the values, and 0 for what cannot be chosen): a round is each lane's best, the DPP
+// maximum over the row, and taking that one out.  (A wavefront a token, with its four keys a lane of
+// 256 experts, spent as many instructions a round on one token: 8192 tokens 22 us.)
 //
 // Grouping is a counting sort, stable, so that equal inputs give equal orders: every block counts
 // its slots per bucket (bucket `count` holds the rows without one), and a second launch adds up the
@@ -33,6 +35,8 @@ constexpr int kMaxExperts = FLEXQ_MAX_EXPERTS;          // buckets: one more
 constexpr int kMaxBlocks = 256;                          // blocks of a launch over many slots: one a CU
 constexpr int kMostSlots = 32768;                        // of a block: its counts are 16 bits
 constexpr int kOneBlock = 1024;                          // slots that one block sorts by itself
+constexpr int kRouteThreads = 512, kRouteWaves = 8;      // of a block of the routing kernel
+constexpr int kRouteTokens = 4 * kRouteWaves;            // ... and what it takes at a time
 
 struct RouteArgs {
     const void *logits;
@@ -40,13 +44,22 @@ struct RouteArgs {
     int M, E, k, sigmoid, groups, top_groups, group_top, renormalise;
     float scale;
     unsigned long long group_inv;   // e / group size = (e * group_inv) >> 32
-    int group_size, group_lanes; // lanes that share a group's scan (a power of two)
+    int group_size, group_shift; // 1 << group_shift lanes share a group's scan
     int32_t *experts;
     float *weights;
     int per_block;               // tokens of a block
     int32_t *order, *offsets;    // one block only, or null
     uint16_t *hist;              // [blocks][pairs_of(E + 1) * 2], or null
 };
+
+// bytes of the routing kernel's tables in LDS: counts, bases, sums, slots
+__host__ __device__ constexpr int route_tables(int buckets)
+{
+    return (((kRouteWaves + 1) * buckets + kRouteWaves + kRouteThreads) * 4 + 15) / 16 * 16;
+}
+
+// place of a token's key e in LDS: a word more in sixteen, so that lanes sixteen or 32 apart meet in no bank
+__host__ __device__ constexpr int padded(int e) { return e + (e >> 4); }
 
 // words of a block's counts, two buckets each
 __host__ __device__ constexpr int pairs_of(int buckets) { return (buckets + 1) / 2; }
@@ -70,14 +83,29 @@ __device__ __forceinline__ float value_of(unsigned key)
     return __uint_as_float(key >> 31 ? key ^ 0x80000000u : ~key);
 }
 
-__device__ __forceinline__ unsigned wave_best(unsigned k) { return wave_max_bits(k); }
-__device__ __forceinline__ unsigned long long wave_best(unsigned long long k)
+// Over the sixteen lanes of a row, every lane with its row's result.
+template <class Op>
+__device__ __forceinline__ unsigned row_all(unsigned v, const Op &op)
 {
-    const unsigned hi = (unsigned)(k >> 32), top = wave_max_bits(hi);
-    const unsigned low = wave_max_bits(hi == top ? (unsigned)k : 0u);
-    return ((unsigned long long)top << 32) | low;
+#define FLEXQ_ROW(ctrl) (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false)
+    v = op(v, FLEXQ_ROW(0x128));      // row_ror:8, 4, 2, 1
+    v = op(v, FLEXQ_ROW(0x124));
+    v = op(v, FLEXQ_ROW(0x122));
+    v = op(v, FLEXQ_ROW(0x121));
+#undef FLEXQ_ROW
+    return v;
 }
-
+__device__ __forceinline__ unsigned row_best(unsigned k)
+{
+    return row_all(k, [](unsigned a, unsigned b) { return max(a, b); });
+}
+template <class Op>
+__device__ __forceinline__ float row_all_f(float v, const Op &op)
+{
+    return __uint_as_float(row_all(__float_as_uint(v), [&](unsigned a, unsigned b) {
+        return __float_as_uint(op(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
 __device__ __forceinline__ double wave_sum(double v)
 {
 #pragma unroll
@@ -85,53 +113,40 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
-// Over the sixteen lanes of a row, every lane with its row's result.
-template <class Op>
-__device__ __forceinline__ float row_all(float v, const Op &op)
+// The best of a row's keys: its index l V + v for lane l of the row (ties: the lowest; -1: there is none), its
+// key in `wins`.  It is taken out.
+template <int V>
+__device__ __forceinline__ int pick(unsigned (&key)[V], int lane, unsigned &wins)
 {
-#define FLEXQ_ROW(ctrl) __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xf, 0xf, false))
-    v = op(v, FLEXQ_ROW(0x128));
-    v = op(v, FLEXQ_ROW(0x124));
-    v = op(v, FLEXQ_ROW(0x4e));
-    v = op(v, FLEXQ_ROW(0xb1));
-#undef FLEXQ_ROW
-    return v;
-}
-
-__device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ unsigned long long uniform(unsigned long long v)
-{
-    return ((unsigned long long)uniform((unsigned)(v >> 32)) << 32) | uniform((unsigned)v);
-}
-
-// The best of the wavefront's keys: its index (ties: the lowest; -1: there is none), its key in `wins`.
-// It is taken out.
-template <int V, class Key>
-__device__ __forceinline__ int pick(Key (&key)[V], int lane, Key &wins)
-{
-    Key best = key[0];
+    unsigned best = key[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) best = max(best, key[v]);
-    wins = uniform(wave_best(best));
-    if (wins == 0) return -1;
-    int e = 64 * V;
+    wins = row_best(best);
+    const unsigned hits = (unsigned)(__ballot(best == wins) >> (lane & 48)) & 0xffffu;
+    const int first = __builtin_ctz(hits | 0x10000u);
+    // (its place in the lane by a minimum over all of them and taken out by number: a chain of "found
+    // already" through the keys is 16 trips to the scalar unit and back)
+    unsigned place[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const unsigned long long at = __ballot(key[v] == wins);
-        if (at) e = min(e, V * (__ffsll(at) - 1) + v);
-    }
+    for (int v = 0; v < V; ++v) place[v] = key[v] == wins ? (unsigned)v : (unsigned)V;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (V * lane == e - v) key[v] = 0;
-    return e;
+    for (int w = 1; w < V; w *= 2)
+#pragma unroll
+        for (int v = 0; v + w < V; v += 2 * w) place[v] = min(place[v], place[v + w]);
+    const unsigned at = (lane & 15) == first ? place[0] : (unsigned)V;
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = at == (unsigned)v ? 0u : key[v];
+    const unsigned found = row_all(at, [](unsigned a, unsigned b) { return min(a, b); });
+    return wins == 0 ? -1 : first * V + (int)found;
 }
 
-// Places of the n <= kThreads slots of a block in the order.  id: this thread's slot's bucket, 0 .. count (have:
-// it has one); wcount: LDS [kWaves][count + 1]; base[b]: LDS, the next free place of bucket b, moved on.
-__device__ void hand_out(int id, bool have, int slot, int count, int *wcount, int *base, int32_t *order)
+// Places of a block's slots, at most one a thread, in the order.  id: this thread's slot's bucket, 0 .. count (have:
+// it has one); wcount: LDS [WAVES][count + 1]; base[b]: LDS, the next free place of bucket b, moved on.
+template <int WAVES>
+__device__ __forceinline__ void hand_out(int id, bool have, int slot, int count, int *wcount, int *base, int32_t *order)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, buckets = count + 1;
-    for (int i = tid; i < kWaves * buckets; i += kThreads) wcount[i] = 0;
+    for (int i = tid; i < WAVES * buckets; i += 64 * WAVES) wcount[i] = 0;
     __syncthreads();
     unsigned long long same = __ballot(have);
     for (int bit = 1; bit <= count; bit <<= 1) {
@@ -141,264 +156,417 @@ __device__ void hand_out(int id, bool have, int slot, int count, int *wcount, in
     const int rank = __popcll(same & ((1ull << lane) - 1ull));
     if (have && rank == 0) wcount[wave * buckets + id] = __popcll(same);
     __syncthreads();
-    if (tid < buckets) {
-        int c[kWaves], at = base[tid];
+    for (int b = tid; b < buckets; b += 64 * WAVES) {
+        int c[WAVES], at = base[b];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) c[w] = wcount[w * buckets + tid];
+        for (int w = 0; w < WAVES; ++w) c[w] = wcount[w * buckets + b];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            wcount[w * buckets + tid] = at;
+        for (int w = 0; w < WAVES; ++w) {
+            wcount[w * buckets + b] = at;
             at += c[w];
         }
-        base[tid] = at;
+        base[b] = at;
     }
     __syncthreads();
     if (have) order[wcount[wave * buckets + id] + rank] = slot;
     __syncthreads();
 }
 
-// base[b] = sum of total[0 .. b - 1] + before[b]; offsets (one block) the sums alone.  One bucket a thread.
-__device__ void begin_buckets(int total, int before, int count, int *base, int *wave_sums, int32_t *offsets)
+// base[b] = sum of total[0 .. b - 1] + before[b]; offsets (one block) the sums alone.  total, before: LDS (before
+// may be null: 0), two buckets a thread.
+template <int WAVES>
+__device__ __forceinline__ void begin_buckets(const int *total, const int *before, int count, int *base, int *wave_sums,
+                                              int32_t *offsets)
 {
+    static_assert(2 * 64 * WAVES > kMaxExperts, "two buckets a thread");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int sum = wave_scan(total);
+    int t[2], b[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool in = 2 * tid + i <= count;
+        t[i] = in ? total[2 * tid + i] : 0;
+        b[i] = in && before ? before[2 * tid + i] : 0;
+    }
+    const int sum = wave_scan(t[0] + t[1]);
     if (lane == 63) wave_sums[wave] = sum;
     __syncthreads();
     int ahead = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const int s = wave_sums[w];
         if (w < wave) ahead += s;
     }
-    const int begin = ahead + sum - total;
-    if (tid <= count) {
-        base[tid] = begin + before;
-        if (offsets) offsets[tid] = begin;               // offsets[count] = the rows that have a bucket
+    int begin = ahead + sum - t[0] - t[1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (2 * tid + i <= count) {
+            base[2 * tid + i] = begin + b[i];
+            if (offsets) offsets[2 * tid + i] = begin;   // offsets[count] = the rows that have a bucket
+        }
+        begin += t[i];
     }
     __syncthreads();
 }
 
 constexpr float kLargest = 3.4028234663852886e38f;
-constexpr float kClose = 0x1p-19f;       // twice the fp32 scores' error, of their size or 1
+constexpr float kClose = 0x1p-20f;       // twice the fp32 scores' error, of their size or 1
 
-// What a wavefront needs to choose for a token: the logits, their largest, and what to do with them.
-template <int V>
-struct Token {
-    float l[V], top;
-};
-
-// Keeps the keys of the top_groups best groups.  key_of_pair: the key of a group from its best two.  Answers
-// whether the first group left out is `near` the last one kept.
-template <int V, class Key, class Pair, class Near>
-__device__ __forceinline__ bool keep_groups(const RouteArgs &a, Key (&key)[V], Key *scratch, int lane,
-                                            const Pair &key_of_pair, const Near &near)
+__device__ __forceinline__ bool near(unsigned above, unsigned below)
 {
-    // the wavefront's keys through its own LDS: lane group g x P lanes scans group g
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (lane * V + v < a.E) scratch[lane * V + v] = key[v];
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    const int P = a.group_lanes, g = lane / P;
-    Key first = 0, second = 0;
-    if (g < a.groups)
-        for (int i = lane % P; i < a.group_size; i += P) {
-            const Key c = scratch[g * a.group_size + i];
-            second = max(second, min(first, c));
-            first = max(first, c);
-        }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read before the next token's keys come)
-    for (int d = 1; d < P; d <<= 1) {
-        const Key f = __shfl_xor(first, d, 64), s = __shfl_xor(second, d, 64);
-        second = max(max(second, s), min(first, f));
-        first = max(first, f);
-    }
-    Key of_group[1] = {lane % P == 0 && g < a.groups && first != 0 ? key_of_pair(first, second) : (Key)0};
-    unsigned long long kept = 0;
-    Key last = 0, next;
-    int win = 0;
-    for (int i = 0; i < a.top_groups; ++i) {
-        win = pick<1>(of_group, lane, next);
-        if (win < 0) break;
-        kept |= 1ull << (win / P);
-        last = next;
-    }
-    const bool unsure = win >= 0 && pick<1>(of_group, lane, next) >= 0 && near(last, next);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const unsigned of = (unsigned)(((unsigned)(lane * V + v) * a.group_inv) >> 32);
-        if (!((kept >> (of & 63)) & 1)) key[v] = 0;
-    }
-    return unsure;
+    const float x = value_of(above), y = value_of(below);
+    return !(x - y > kClose * fmaxf(1.0f, fmaxf(fabsf(x), fabsf(y))));
 }
 
-// The k best by c in 64 bits; lane j answers with the j-th.
-template <int V>
-__device__ __forceinline__ int choose_exactly(const RouteArgs &a, const Token<V> &t, void *scratch, int lane)
+// Keeps the keys of the top_groups best groups.  key_of_pair: the key of a group from its best two; unsure: set
+// where the first group left out is `close` to the last one kept.  G: groups a lane of the row keeps (1: up to 16
+// groups, each scanned by as many lanes as there are for it).
+template <int V, int G, class Pair, class Close>
+__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane,
+                                            const Pair &key_of_pair, const Close &close, bool &unsure)
 {
+    const int l = lane & 15;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (l * V + v < a.E) scratch[padded(l * V + v)] = key[v];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (a wavefront's own part of LDS: no barrier)
+    const int shift = G == 1 ? a.group_shift : 0, P = 1 << shift;     // P lanes a group
+    unsigned of_group[G];
+#pragma unroll
+    for (int q = 0; q < G; ++q) {
+        const int g = G == 1 ? l >> shift : l * G + q;
+        unsigned first = 0, second = 0;
+        if (g < a.groups)
+            for (int i = l & (P - 1); i < a.group_size; i += P) {
+                const unsigned c = scratch[padded(g * a.group_size + i)];
+                second = max(second, min(first, c));
+                first = max(first, c);
+            }
+        if (G == 1)
+            for (int d = 1; d < P; d <<= 1) {
+                const unsigned f = __shfl_xor(first, d, 64), s = __shfl_xor(second, d, 64);
+                second = max(max(second, s), min(first, f));
+                first = max(first, f);
+            }
+        of_group[q] = (l & (P - 1)) == 0 && first != 0 ? key_of_pair(first, second) : 0u;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read before the next tokens' keys come)
+    unsigned long long kept = 0;
+    unsigned last = 0, next;
+    for (int i = 0; i < a.top_groups; ++i) {
+        const int g = pick(of_group, lane, next);
+        if (g >= 0) kept |= 1ull << (g >> shift);
+        last = next;
+    }
+    pick(of_group, lane, next);
+    if (last != 0 && next != 0 && close(last, next)) unsure = true;
+    if ((a.group_size & (V - 1)) == 0) {                     // a lane's experts are of one group
+        const unsigned of = (unsigned)(((unsigned)(l * V) * a.group_inv) >> 32);
+        const bool in = (kept >> (of & 63)) & 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = in ? key[v] : 0;
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const unsigned of = (unsigned)(((unsigned)(l * V + v) * a.group_inv) >> 32);
+            if (!((kept >> (of & 63)) & 1)) key[v] = 0;
+        }
+    }
+}
+template <int V, class Pair, class Close>
+__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane,
+                                            const Pair &key_of_pair, const Close &close, bool &unsure)
+{
+    if (a.groups <= 16)
+        keep_groups<V, 1>(a, key, scratch, lane, key_of_pair, close, unsure);
+    else
+        keep_groups<V, 4>(a, key, scratch, lane, key_of_pair, close, unsure);
+}
+
+// The best of a whole wavefront's 64-bit keys, as pick() above: its index l V + v for lane l.
+template <int V>
+__device__ __forceinline__ int pick_wide(unsigned long long (&key)[V], int lane, unsigned long long &wins)
+{
+    unsigned long long best = key[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) best = max(best, key[v]);
+    const unsigned hi = (unsigned)(best >> 32), top = wave_max_bits(hi);
+    const unsigned low = wave_max_bits(hi == top ? (unsigned)best : 0u);
+    wins = ((unsigned long long)top << 32) | low;
+    if (wins == 0) return -1;
+    const int first = __ffsll((unsigned long long)__ballot(best == wins)) - 1;
+    int at = 0;
+#pragma unroll
+    for (int v = V - 1; v >= 0; --v)
+        if (key[v] == wins) at = v;
+    const int e = first * V + __builtin_amdgcn_readlane(at, first);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (V * lane == e - v) key[v] = 0;
+    return e;
+}
+
+// One token's k best by c in 64 bits, a wavefront on it: lane j answers with the j-th.  scratch: the wavefront's
+// part of LDS, 8 E bytes of it.
+template <int V, class Logit>
+__device__ __forceinline__ int choose_exactly(const RouteArgs &a, const Logit &logit, unsigned long long *scratch, int lane)
+{
+    float x[V], top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        x[v] = lane * V + v < a.E ? logit(lane * V + v) : -INFINITY;
+        top = fmaxf(top, x[v]);
+    }
+    top = wave_max(top);
     double total = 1.0;
     if (!a.sigmoid) {
-        double sum = 0.0;
+        total = 0.0;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (t.l[v] > -INFINITY) sum += exp((double)t.l[v] - (double)t.top);
-        total = wave_sum(sum);
+            if (x[v] > -INFINITY) total += exp((double)x[v] - (double)top);
+        total = wave_sum(total);
     }
-    unsigned long long key[V];
+    unsigned long long key[V], wins;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         key[v] = 0;
-        if (t.l[v] > -INFINITY) {
-            const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)t.l[v])) : exp((double)t.l[v] - (double)t.top) / total;
+        if (x[v] > -INFINITY) {
+            const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)x[v])) : exp((double)x[v] - (double)top) / total;
             const double c = a.bias ? s + (double)a.bias[lane * V + v] : s;
             if (c > -INFINITY) key[v] = key_of(c);
         }
     }
-    if (a.top_groups < a.groups)
-        keep_groups(a, key, static_cast<unsigned long long *>(scratch), lane,
-                    [&](unsigned long long f, unsigned long long s) {
-                        return a.group_top == 2 && s != 0 ? key_of(value_of(f) + value_of(s)) : f;
-                    },
-                    [](unsigned long long, unsigned long long) { return false; });
+    if (a.top_groups < a.groups) {                           // a lane scans a group
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (lane * V + v < a.E) scratch[lane * V + v] = key[v];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        unsigned long long first = 0, second = 0, worth[1];
+        if (lane < a.groups)
+            for (int i = 0; i < a.group_size; ++i) {
+                const unsigned long long c = scratch[lane * a.group_size + i];
+                second = max(second, min(first, c));
+                first = max(first, c);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        worth[0] = a.group_top == 2 && second != 0 ? key_of(value_of(first) + value_of(second)) : first;
+        unsigned long long kept = 0;
+        for (int j = 0; j < a.top_groups; ++j) {
+            const int g = pick_wide(worth, lane, wins);
+            if (g >= 0) kept |= 1ull << g;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (!((kept >> (((unsigned)(lane * V + v) * a.group_inv >> 32) & 63)) & 1)) key[v] = 0;
+    }
     int mine = -1;
     for (int j = 0; j < a.k; ++j) {
-        unsigned long long wins;
-        const int e = pick(key, lane, wins);
-        if (e < 0) break;
+        const int e = pick_wide(key, lane, wins);
         if (lane == j) mine = e;
     }
     return mine;
 }
 
+// Up to sixteen experts, a lane each (mine; -1: none), put in the order of their c in 64 bits.
+__device__ __forceinline__ int order_exactly(const RouteArgs &a, float lv, int mine, int lane)
+{
+    double c = -INFINITY;
+    if (mine >= 0) {
+        c = 1.0 / (1.0 + exp(-(double)lv));
+        if (a.bias) c += (double)a.bias[mine];
+    }
+    const long long bits = __double_as_longlong(c);
+    int rank = 0;
+#pragma unroll
+    for (int d = 1; d < 16; ++d) {
+        const int from = (lane & 48) | ((lane + d) & 15);
+        const unsigned lo = (unsigned)__shfl((int)(unsigned)bits, from, 64), hi = (unsigned)__shfl((int)(bits >> 32), from, 64);
+        const double other = __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));
+        const int e = __shfl(mine, from, 64);
+        // (lanes without one stay behind the others, in their order)
+        const bool ahead = e >= 0 && (mine < 0 || other > c || (other == c && e < mine));
+        rank += ahead || (e < 0 && mine < 0 && (from & 15) < (lane & 15)) ? 1 : 0;
+    }
+    return __builtin_amdgcn_ds_permute(4 * ((lane & 48) | rank), mine);
+}
+
 // BY_LOGIT: the logits are compared; else c.
 template <bool BY_LOGIT, int V, bool HALF>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a)
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = a.E, k = a.k, buckets = E + 1;
-    int *hist = reinterpret_cast<int *>(lds);                          // [kWaves][buckets] or [buckets]
-    int *base = hist + kWaves * buckets;                               // [buckets]
-    int *wave_sums = base + buckets;                                   // [kWaves]
-    int *ids = wave_sums + kWaves;                                     // [kOneBlock]
-    unsigned char *scratch = lds + ((size_t)((kWaves + 1) * buckets + kWaves + kOneBlock) * 4 + 15) / 16 * 16 +
-                             (size_t)wave * E * (BY_LOGIT ? 4 : 8);
+    const int l = lane & 15, row = lane >> 4;
+    int *hist = reinterpret_cast<int *>(lds);                          // [kRouteWaves][buckets] or [buckets]
+    int *base = hist + kRouteWaves * buckets;                          // [buckets]
+    int *wave_sums = base + buckets;                                   // [kRouteWaves]
+    int *ids = wave_sums + kRouteWaves;                                // [kRouteThreads]
+    const int stride = padded(E);                                      // words of a token's keys
+    unsigned *scratch = reinterpret_cast<unsigned *>(lds + route_tables(buckets)) + (size_t)(4 * wave + row) * stride;
     const bool grouping = a.hist || a.order;
     if (grouping) {
-        for (int i = tid; i < buckets; i += kThreads) hist[i] = 0;
+        for (int i = tid; i < buckets; i += kRouteThreads) hist[i] = 0;
         __syncthreads();
     }
     float bias[V];
     if constexpr (!BY_LOGIT) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) bias[v] = a.bias && lane * V + v < E ? a.bias[lane * V + v] : 0.0f;
+        for (int v = 0; v < V; ++v) bias[v] = 0.0f;
+        if (a.bias)
+#pragma unroll
+            for (int v = 0; v < V; ++v) bias[v] = a.bias[min(l * V + v, E - 1)];
     }
 
     const int m0 = blockIdx.x * a.per_block, m1 = min(a.M, m0 + a.per_block);
-    for (int m = m0 + wave; m < m1; m += kWaves) {
-        const uint16_t *half = static_cast<const uint16_t *>(a.logits) + (size_t)m * E;
-        const float *full = static_cast<const float *>(a.logits) + (size_t)m * E;
-        Token<V> t;
-        if (E % V == 0) {                                    // (rows begin on a multiple of V)
-            typedef float Floats __attribute__((ext_vector_type(V)));
-            typedef uint16_t Halves __attribute__((ext_vector_type(V)));
+    for (int step = m0; step < m1; step += kRouteTokens) {
+        const int m = step + 4 * wave + row;
+        if (step + 4 * wave >= m1) break;                    // (the wavefront's first token: uniform)
+        const bool here = m < m1;
+        const uint16_t *half = static_cast<const uint16_t *>(a.logits) + (size_t)(here ? m : m0) * E;
+        const float *full = static_cast<const float *>(a.logits) + (size_t)(here ? m : m0) * E;
+        float x[V], top = -INFINITY;
+        // (no branches and no more code than it takes: a wavefront passes here once or twice, and what it waits for
+        // is the instructions)
+        constexpr int W = V < 4 ? V : 4;
+        if (E % W == 0) {                                    // W logits a load (rows begin on a multiple of W)
+            typedef float Floats __attribute__((ext_vector_type(W)));
+            typedef uint16_t Halves __attribute__((ext_vector_type(W)));
 #pragma unroll
-            for (int v = 0; v < V; ++v) t.l[v] = -INFINITY;
-            if (lane * V < E) {
+            for (int v0 = 0; v0 < V; v0 += W) {
+                const int e = min(l * V + v0, E - W);
                 if constexpr (HALF) {
-                    const Halves h = *reinterpret_cast<const Halves *>(half + lane * V);
+                    const Halves h = *reinterpret_cast<const Halves *>(half + e);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) t.l[v] = h2f(h[v]);
+                    for (int i = 0; i < W; ++i) x[v0 + i] = h2f(h[i]);
                 } else {
-                    const Floats f = *reinterpret_cast<const Floats *>(full + lane * V);
+                    const Floats f = *reinterpret_cast<const Floats *>(full + e);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) t.l[v] = f[v];
+                    for (int i = 0; i < W; ++i) x[v0 + i] = f[i];
                 }
             }
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                t.l[v] = lane * V + v < E ? (HALF ? h2f(half[lane * V + v]) : full[lane * V + v]) : -INFINITY;
+            for (int v = 0; v < V; ++v) {
+                const int e = min(l * V + v, E - 1);
+                x[v] = HALF ? h2f(half[e]) : full[e];
+            }
         }
-        t.top = -INFINITY;
+        const int valid = here ? E - l * V : 0;              // of this lane's keys
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            t.l[v] = t.l[v] > -INFINITY ? fminf(t.l[v], kLargest) : -INFINITY;   // NaN: cannot be chosen
-            t.top = fmaxf(t.top, t.l[v]);
+            x[v] = v < valid && x[v] > -INFINITY ? fminf(x[v], kLargest) : -INFINITY;   // NaN: cannot be chosen
+            top = fmaxf(top, x[v]);
         }
         float total = 1.0f;                                  // of the softmax, where it is needed
         if (!a.sigmoid && (!BY_LOGIT || !a.renormalise)) {
-            t.top = wave_max(t.top);
+            top = row_all_f(top, [](float p, float q) { return fmaxf(p, q); });
             float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += t.l[v] > -INFINITY ? expf(t.l[v] - t.top) : 0.0f;
-            total = wave_sum(sum);
+            for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? expf(x[v] - top) : 0.0f;
+            total = row_all_f(sum, [](float p, float q) { return p + q; });
         }
         unsigned key[V];
+        if constexpr (BY_LOGIT) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            key[v] = 0;
-            if (t.l[v] > -INFINITY) {
-                if constexpr (BY_LOGIT) {
-                    key[v] = key_of(t.l[v]);
-                } else {
-                    const float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t.l[v] * -1.44269504088896341f))
-                                              : __builtin_amdgcn_exp2f((t.l[v] - t.top) * 1.44269504088896341f) *
-                                                    __builtin_amdgcn_rcpf(total);
-                    const float c = s + bias[v];
-                    if (c > -INFINITY) key[v] = key_of(c);
+            for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY ? key_of(x[v]) : 0u;
+        } else {
+            // (of -inf: a score of 0, and no key)
+            constexpr float kLog2e = 1.44269504088896341f;
+            float c[V];
+            if (a.sigmoid) {
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    c[v] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[v] * -kLog2e)) + bias[v];
+            } else {
+                const float part = __builtin_amdgcn_rcpf(total);
+#pragma unroll
+                for (int v = 0; v < V; ++v) c[v] = __builtin_amdgcn_exp2f((x[v] - top) * kLog2e) * part + bias[v];
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY && c[v] > -INFINITY ? key_of(c[v]) : 0u;
+        }
+        bool unsure = false;                                 // all the experts have to be looked at in 64 bits
+        if (a.top_groups < a.groups)
+            keep_groups(a, key, scratch, lane,
+                        [&](unsigned f, unsigned s) {
+                            return !BY_LOGIT && a.group_top == 2 && s != 0 ? key_of(value_of(f) + value_of(s)) : f;
+                        },
+                        [](unsigned p, unsigned q) {         // (sums of two: twice as far)
+                            return !BY_LOGIT && near(key_of(0.5f * value_of(p)), key_of(0.5f * value_of(q)));
+                        },
+                        unsure);
+        int mine = -1;                                       // the expert of slot l
+        unsigned last = 0, wins = 0;
+        bool close = false;                                  // two that follow each other are
+        // the k best and, where c is good to fp32 only, whoever is close behind the last of them
+        bool behind = true;
+        for (int j = 0;; ++j) {
+            if (BY_LOGIT && j == k) break;
+            const int e = pick(key, lane, wins);
+            if (!BY_LOGIT && j > 0) {
+                const bool follows = last != 0 && wins != 0 && near(last, wins);
+                if (j >= k) {
+                    behind = behind && follows;
+                    if (__ballot(behind) == 0) break;
+                }
+                close |= j >= k ? behind : follows;
+                if (j == 16) {
+                    unsure |= behind;
+                    break;
                 }
             }
-        }
-        auto near = [](unsigned above, unsigned below) {
-            const float x = value_of(above), y = value_of(below);
-            return !(x - y > kClose * fmaxf(1.0f, fmaxf(fabsf(x), fabsf(y))));
-        };
-        bool unsure = false;
-        if (a.top_groups < a.groups)
-            unsure = keep_groups(a, key, reinterpret_cast<unsigned *>(scratch), lane,
-                                 [&](unsigned f, unsigned s) {
-                                     return !BY_LOGIT && a.group_top == 2 && s != 0 ? key_of(value_of(f) + value_of(s)) : f;
-                                 },
-                                 [&](unsigned x, unsigned y) { return near(key_of(0.5f * value_of(x)), key_of(0.5f * value_of(y))); });
-        int mine = -1;                                       // the expert of slot `lane`, and its key
-        unsigned won = 0;
-        for (int j = 0; j < (BY_LOGIT ? k : k + 1); ++j) {
-            unsigned wins;
-            const int e = pick(key, lane, wins);
-            if (e < 0) break;
-            if (lane == j) {
-                mine = e;
-                if (!BY_LOGIT) won = wins;
-            }
+            if (l == j && (j < k || behind)) mine = e;
+            last = wins;
         }
         if constexpr (!BY_LOGIT) {
-            const unsigned next = __shfl_down(won, 1, 64);
-            unsure |= __ballot(lane < k && next != 0 && near(won, next)) != 0;
-            if (unsure) mine = choose_exactly<V>(a, t, scratch, lane);
+            unsure |= close && !a.sigmoid;
+            if (__ballot(unsure) != 0) {
+                for (int r = 0; r < 4; ++r) {                // one token after the other
+                    if (!((__ballot(unsure) >> (16 * r)) & 0xffffu)) continue;
+                    const int of = step + 4 * wave + r;      // (a token that is there: it had something to choose)
+                    const int chosen = choose_exactly<(V + 3) / 4>(
+                        a,
+                        [&](int e) {
+                            const size_t at = (size_t)of * E + e;
+                            const float v = HALF ? h2f(static_cast<const uint16_t *>(a.logits)[at]) : static_cast<const float *>(a.logits)[at];
+                            return v > -INFINITY ? fminf(v, kLargest) : -INFINITY;
+                        },
+                        reinterpret_cast<unsigned long long *>(scratch - (size_t)row * stride), lane);
+                    const int mine_now = __shfl(chosen, l, 64);
+                    if (row == r) mine = mine_now;
+                }
+                close = close && !unsure;
+            }
+            if (__ballot(close)) {
+                float lv = 0.0f;
+                if (mine >= 0) lv = fminf(HALF ? h2f(half[mine]) : full[mine], kLargest);
+                const int ordered = order_exactly(a, lv, mine, lane);
+                if (close) mine = ordered;
+            }
         }
 
-        // weights, in the lanes of the first row: softmax renormalised from the largest of the chosen, so that
-        // nothing underflows; sigmoids that all lie far below 0 are exponentials there
-        const bool chosen = lane < k && mine >= 0;
+        // weights: softmax renormalised from the largest of the chosen, so that nothing underflows; sigmoids that
+        // all lie far below 0 are exponentials there
+        const bool chosen = l < k && mine >= 0;
         float lv = -INFINITY;
         if (chosen) lv = fminf(HALF ? h2f(half[mine]) : full[mine], kLargest);
-        const float above = row_all(lv, [](float x, float y) { return fmaxf(x, y); });
+        const float above = row_all_f(lv, [](float p, float q) { return fmaxf(p, q); });
         float w = 0.0f;
         if (chosen) {
             if (a.renormalise && (!a.sigmoid || above < -60.0f))
                 w = expf(lv - above);
             else
-                w = a.sigmoid ? 1.0f / (1.0f + expf(-lv)) : expf(lv - t.top) / total;
+                w = a.sigmoid ? 1.0f / (1.0f + expf(-lv)) : expf(lv - top) / total;
         }
         if (a.renormalise) {
-            const float sum = row_all(w, [](float x, float y) { return x + y; });
+            const float sum = row_all_f(w, [](float p, float q) { return p + q; });
             w = sum > 0.0f ? w / sum : 0.0f;
         }
-        if (lane < k) {
-            a.experts[(size_t)m * k + lane] = mine;
-            a.weights[(size_t)m * k + lane] = w * a.scale;
+        if (here && l < k) {
+            a.experts[(size_t)m * k + l] = mine;
+            a.weights[(size_t)m * k + l] = w * a.scale;
             if (grouping) {
                 const int bucket = mine < 0 ? E : mine;
-                if (a.order) ids[(m - m0) * k + lane] = bucket;
+                if (a.order) ids[(m - m0) * k + l] = bucket;
                 atomicAdd(&hist[bucket], 1);
             }
         }
@@ -407,14 +575,14 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a)
     __syncthreads();
     if (a.hist) {
         const int pairs = pairs_of(buckets);
-        for (int i = tid; i < pairs; i += kThreads)
+        for (int i = tid; i < pairs; i += kRouteThreads)
             reinterpret_cast<unsigned *>(a.hist)[(size_t)blockIdx.x * pairs + i] =
                 (unsigned)hist[2 * i] | (2 * i + 1 < buckets ? (unsigned)hist[2 * i + 1] << 16 : 0u);
         return;
     }
-    begin_buckets(tid < buckets ? hist[tid] : 0, 0, E, base, wave_sums, a.offsets);
+    begin_buckets<kRouteWaves>(hist, nullptr, E, base, wave_sums, a.offsets);
     const bool have = tid < (m1 - m0) * k;
-    hand_out(have ? ids[tid] : 0, have, tid, E, hist, base, a.order);
+    hand_out<kRouteWaves>(have ? ids[tid] : 0, have, tid, E, hist, base, a.order);
 }
 
 // Counts of a block's rows; ids outside 0 .. count - 1 belong to none.
@@ -484,11 +652,10 @@ __global__ __launch_bounds__(kThreads) void place_kernel(const int32_t *ids, int
         if (tid < n) atomicAdd(&total[(unsigned)id < (unsigned)count ? id : count], 1);
     }
     __syncthreads();
-    const int all = tid < buckets ? total[tid] : 0, ahead = tid < buckets ? before[tid] : 0;
-    begin_buckets(all, ahead, count, base, wave_sums, blockIdx.x == 0 ? offsets : nullptr);
+    begin_buckets<kWaves>(total, before, count, base, wave_sums, blockIdx.x == 0 ? offsets : nullptr);
     for (int c0 = 0; c0 < n; c0 += kThreads) {
         if (c0 > 0) id = c0 + tid < n ? ids[s0 + c0 + tid] : 0;
-        hand_out((unsigned)id < (unsigned)count ? id : count, c0 + tid < n, s0 + c0 + tid, count, wcount, base, order);
+        hand_out<kWaves>((unsigned)id < (unsigned)count ? id : count, c0 + tid < n, s0 + c0 + tid, count, wcount, base, order);
     }
 }
 
@@ -500,7 +667,7 @@ inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3
 int rows_per_block(int rows, int unit)
 {
     int per = (rows + kMaxBlocks - 1) / kMaxBlocks;
-    const int wanted = unit == 0 ? kThreads : kWaves;    // a slot a thread, a token a wavefront
+    const int wanted = unit == 0 ? kThreads : kRouteTokens / 2;    // a slot a thread; four wavefronts' tokens
     if (unit == 0) unit = 1;
     per = per > wanted ? per : wanted;
     return per < kMostSlots / unit ? per : kMostSlots / unit;
@@ -520,24 +687,27 @@ hipError_t launch_place(const int32_t *ids, int rows, int per_block, int count, 
 template <bool BY_LOGIT, int V>
 hipError_t launch_route_v(const RouteArgs &a, bool half, unsigned blocks, hipStream_t st)
 {
-    constexpr int bytes = BY_LOGIT ? 4 : 8;              // of a key in LDS
-    const size_t lds = (size_t)(lds_of(a.E + 1) + (a.top_groups < a.groups ? kWaves * a.E * bytes : 0));
+    // the keys of a block's tokens; four tokens' part holds one's in 64 bits
+    const size_t lds = (size_t)(route_tables(a.E + 1) + (a.top_groups < a.groups ? kRouteTokens * padded(a.E) * 4 + 64 : 0));
     static std::atomic<unsigned long long> allowed[2];
     auto kern = half ? route_kernel<BY_LOGIT, V, true> : route_kernel<BY_LOGIT, V, false>;
-    constexpr int most = ((kWaves + 1) * (kMaxExperts + 1) + kWaves + kOneBlock) * 4 + 16 + kWaves * kMaxExperts * bytes;
+    constexpr int most = route_tables(kMaxExperts + 1) + kRouteTokens * padded(kMaxExperts) * 4 + 64;
+    static_assert(most <= 160 * 1024, "LDS of one CU");
     if (hipError_t e = flexq::allow_dynamic_lds(reinterpret_cast<const void *>(kern), most, allowed[half]); e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL(kern, dim3(blocks), dim3(kRouteThreads), lds, st, a);
     return hipGetLastError();
 }
 
 template <bool BY_LOGIT>
 hipError_t launch_route(const RouteArgs &a, bool half, unsigned blocks, hipStream_t st)
 {
-    if (a.E <= 64) return launch_route_v<BY_LOGIT, 1>(a, half, blocks, st);
-    if (a.E <= 128) return launch_route_v<BY_LOGIT, 2>(a, half, blocks, st);
-    if (a.E <= 256) return launch_route_v<BY_LOGIT, 4>(a, half, blocks, st);
-    return launch_route_v<BY_LOGIT, 8>(a, half, blocks, st);
+    if (a.E <= 16) return launch_route_v<BY_LOGIT, 1>(a, half, blocks, st);
+    if (a.E <= 32) return launch_route_v<BY_LOGIT, 2>(a, half, blocks, st);
+    if (a.E <= 64) return launch_route_v<BY_LOGIT, 4>(a, half, blocks, st);
+    if (a.E <= 128) return launch_route_v<BY_LOGIT, 8>(a, half, blocks, st);
+    if (a.E <= 256) return launch_route_v<BY_LOGIT, 16>(a, half, blocks, st);
+    return launch_route_v<BY_LOGIT, 32>(a, half, blocks, st);
 }
 
 size_t hist_bytes(int rows, int unit, int count)
@@ -614,14 +784,14 @@ flexq_status flexq_route(const void *logits, int half, int M, int E, const flexq
     a.scale = R->scale;
     a.group_size = E / R->groups;
     a.group_inv = (1ull << 32) / (unsigned)a.group_size + 1;
-    a.group_lanes = 64;
-    while (64 / a.group_lanes < R->groups) a.group_lanes /= 2;
+    a.group_shift = 4;
+    while (a.group_shift > 0 && (16 >> a.group_shift) < R->groups) --a.group_shift;
     a.experts = experts;
     a.weights = weights;
     a.per_block = rows_per_block(M, R->k);
-    // two tokens a wavefront, and the places, in one launch: at 64 tokens 11.4 us, in two 8.9
-    static_assert(2 * kWaves * FLEXQ_MAX_EXPERTS_PER_TOKEN <= kOneBlock, "a block's slots");
-    const bool one = M <= 2 * kWaves;
+    // what a block takes at a time, and the places, in one launch
+    static_assert(kRouteTokens * FLEXQ_MAX_EXPERTS_PER_TOKEN <= kRouteThreads, "a slot a thread");
+    const bool one = M <= kRouteTokens;
     if (order) {
         if (!one && (!workspace || workspace_bytes < hist_bytes(M, R->k, E))) return FLEXQ_EWORKSPACE;
         if (!one && !aligned16(workspace)) return FLEXQ_EALIGN;
