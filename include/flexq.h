@@ -373,7 +373,7 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
 /*
  * Rows that choose their own weights: experts, and the adapters of many requests.
  *
- * A GROUPING of `rows` rows over `count` groups (at most FLEXQ_MAX_EXPERTS) is two device arrays:
+ * A GROUPING of `rows` rows (at most 2^28) over `count` groups (at most FLEXQ_MAX_EXPERTS) is two device arrays:
  *   order    int32 [rows]       every row once: those of group 0, then group 1, ..., each group's in
  *                               ascending order, and last the rows of no group
  *   offsets  int32 [count + 1]  group g is order[offsets[g]] .. order[offsets[g + 1] - 1]; offsets[0] = 0,
@@ -398,8 +398,8 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *   order, offsets  dev, out, or both NULL: the grouping of the M k slots (slot m k + j) over the E experts
  *   workspace       as for flexq_group_rows, flexq_route_workspace_bytes(M, E, k); may be NULL without order
  *                   and for up to 32 tokens
- * c is made and compared in 64 bits where a bias or a sum enters it, and the logits themselves are
- * compared where none does; weights are good to a few ulp of fp32.
+ * The choice is that of c in 64 bits where a bias or a sum enters it, and of the logits themselves where none does;
+ * weights are good to a few ulp of fp32, also where the scores themselves underflow (sigmoids far below zero).
  * 1 <= k <= FLEXQ_MAX_EXPERTS_PER_TOKEN, k <= top_groups * E / groups, groups <= 64, 0 < scale < inf.
  *
  * flexq_expert_linear: the linear layer (flexq_gemm_w6a6 / _w6a8, codes of either width) of E experts on

@@ -458,19 +458,22 @@ def _here(t, dtype, shape, dev):
     return t
 
 
-def _scratch(nbytes, given, device):
+def _scratch(nbytes, given, device, cur):
     if nbytes == 0:
         raise FlexQError("flexq: invalid shape for workspace")
-    return given if given is not None else torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if given is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _here(given, torch.uint8, given.shape, cur)
 
 
 def group_rows(ids, count, workspace=None):
     """int32 ids (any shape; outside 0 .. count - 1: no group) -> (order, offsets): the rows by group, each
     group's in ascending order, those without one last, and where each group begins."""
     lib = load()
-    _here(ids, torch.int32, ids.shape, _current(ids))
+    cur = _current(ids)
+    _here(ids, torch.int32, ids.shape, cur)
     rows, dev = ids.numel(), ids.device
-    ws = _scratch(lib.flexq_group_rows_workspace_bytes(rows, count), workspace, dev)
+    ws = _scratch(lib.flexq_group_rows_workspace_bytes(rows, count), workspace, dev, cur)
     order = torch.empty(rows, dtype=torch.int32, device=dev)
     offsets = torch.empty(count + 1, dtype=torch.int32, device=dev)
     _check(lib.flexq_group_rows(ids.data_ptr(), rows, count, order.data_ptr(), offsets.data_ptr(), ws.data_ptr(), ws.numel(),
@@ -496,14 +499,12 @@ def route_experts(logits, k, score="softmax", bias=None, groups=1, top_groups=1,
         _here(bias, torch.float32, (E,), cur)
     dev = logits.device
     r = _Routing(k, kind, groups, top_groups, group_top, 1 if renormalise else 0, scale, None if bias is None else bias.data_ptr())
-    nbytes = lib.flexq_route_workspace_bytes(M, E, k)
-    if nbytes == 0:
-        raise FlexQError("flexq: invalid number of tokens, experts or experts a token")
-    experts = torch.empty((M, k), dtype=torch.int32, device=dev)
-    weights = torch.empty((M, k), dtype=torch.float32, device=dev)
+    experts = torch.empty(M, k, dtype=torch.int32, device=dev)
+    weights = torch.empty(M, k, dtype=torch.float32, device=dev)
     order = offsets = ws = None
     if group:
-        ws = workspace if workspace is not None or M <= _ROUTE_ONE_LAUNCH else torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        if workspace is not None or M > _ROUTE_ONE_LAUNCH:
+            ws = _scratch(lib.flexq_route_workspace_bytes(M, E, k), workspace, dev, cur)
         order = torch.empty(M * k, dtype=torch.int32, device=dev)
         offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
     _check(lib.flexq_route(logits.data_ptr(), 1 if dtype == torch.float16 else 0, M, E, ctypes.byref(r), experts.data_ptr(),
@@ -572,7 +573,7 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
     _here(y, half, (M, N), cur)
     _here(order, i32, (M,), cur)
     _here(offsets, i32, (L + 1,), cur)
-    ws = _scratch(lib.flexq_adapters_workspace_bytes(M, L, R, K), workspace, x.device)
+    ws = _scratch(lib.flexq_adapters_workspace_bytes(M, L, R, K), workspace, x.device, cur)
     res = torch.empty((M, N), dtype=half, device=x.device) if out is None else _here(out, half, (M, N), cur)
     _check(lib.flexq_adapters(a.data_ptr(), b.data_ptr(), scale.data_ptr(), L, R, x.data_ptr(), order.data_ptr(),
                               offsets.data_ptr(), M, N, K, y.data_ptr(), res.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))

@@ -363,14 +363,15 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
     p.columns = up_columns(pieces_likely(M, L + rest, height), N, tiles, blocks);
     hipStream_t st = (hipStream_t)stream;
     const int rt = tiles == 1 ? 1 : tiles == 2 ? 2 : 4, chunks = (tiles + rt - 1) / rt;
-    const unsigned down_grid = (unsigned)(pieces_bound(M, L, height) * chunks * p.splits);
-    const unsigned up_grid = (unsigned)(pieces_bound(M, L + rest, height) * ((N + p.columns - 1) / p.columns));
+    const long down_grid = pieces_bound(M, L, height) * chunks * p.splits;
+    const long up_grid = pieces_bound(M, L + rest, height) * ((N + p.columns - 1) / p.columns);
+    if (down_grid >= (1L << 31) || up_grid >= (1L << 31)) return FLEXQ_ESHAPE;
     auto down = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(down_grid), dim3(256), 0, st, p, chunks);
+        hipLaunchKernelGGL(kern, dim3((unsigned)down_grid), dim3(256), 0, st, p, chunks);
         return hipGetLastError();
     };
     auto up = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(up_grid), dim3(256), 0, st, p, rest);
+        hipLaunchKernelGGL(kern, dim3((unsigned)up_grid), dim3(256), 0, st, p, rest);
         return hipGetLastError();
     };
     hipError_t e;

@@ -33,6 +33,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxExperts = FLEXQ_MAX_EXPERTS;          // buckets: one more
 constexpr int kMaxBlocks = 256;                          // blocks of a launch over many slots: one a CU
+constexpr int kMostRows = 1 << 28;                       // every block reads all blocks' counts: 8192 of them
 constexpr int kMostSlots = 32768;                        // of a block: its counts are 16 bits
 constexpr int kOneBlock = 1024;                          // slots that one block sorts by itself
 constexpr int kRouteThreads = 512, kRouteWaves = 8;      // of a block of the routing kernel
@@ -459,10 +460,19 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
         float total = 1.0f;                                  // of the softmax, where it is needed
         if (!a.sigmoid && (!BY_LOGIT || !a.renormalise)) {
             top = row_all_f(top, [](float p, float q) { return fmaxf(p, q); });
-            float sum = 0.0f;
+            if constexpr (BY_LOGIT) {
+                float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? expf(x[v] - top) : 0.0f;
-            total = row_all_f(sum, [](float p, float q) { return p + q; });
+                for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? expf(x[v] - top) : 0.0f;
+                total = row_all_f(sum, [](float p, float q) { return p + q; });
+            } else {                     // in 64 bits: the roundings of 512 additions would be more than c may be off by
+                double sum = 0.0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? (double)expf(x[v] - top) : 0.0;
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+                total = (float)sum;
+            }
         }
         unsigned key[V];
         if constexpr (BY_LOGIT) {
@@ -724,7 +734,7 @@ extern "C" {
 
 size_t flexq_group_rows_workspace_bytes(int rows, int count)
 {
-    if (rows < 1 || count < 1 || count > kMaxExperts) return 0;
+    if (rows < 1 || rows > kMostRows || count < 1 || count > kMaxExperts) return 0;
     return hist_bytes(rows, 0, count);
 }
 
@@ -732,7 +742,7 @@ flexq_status flexq_group_rows(const int32_t *ids, int rows, int count, int32_t *
                               void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!ids || !order || !offsets || rows < 1 || count < 1) return FLEXQ_EINVAL;
-    if (count > kMaxExperts) return FLEXQ_ESHAPE;
+    if (count > kMaxExperts || rows > kMostRows) return FLEXQ_ESHAPE;
     if (!aligned4(ids) || !aligned4(order) || !aligned4(offsets)) return FLEXQ_EALIGN;
     if (!workspace || workspace_bytes < hist_bytes(rows, 0, count)) return FLEXQ_EWORKSPACE;
     if (!aligned16(workspace)) return FLEXQ_EALIGN;
@@ -749,7 +759,9 @@ flexq_status flexq_group_rows(const int32_t *ids, int rows, int count, int32_t *
 
 size_t flexq_route_workspace_bytes(int M, int E, int k)
 {
-    if (M < 1 || E < 1 || E > kMaxExperts || k < 1 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN || k > E) return 0;
+    if (M < 1 || E < 1 || E > kMaxExperts || k < 1 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN || k > E ||
+        (long)M * k > kMostRows)
+        return 0;
     return hist_bytes(M, k, E);
 }
 
@@ -766,7 +778,7 @@ flexq_status flexq_route(const void *logits, int half, int M, int E, const flexq
     if (R->top_groups < 1 || R->top_groups > R->groups || R->group_top < 1 || R->group_top > 2) return FLEXQ_EINVAL;
     if ((long)R->k > (long)(E / R->groups) * R->top_groups) return FLEXQ_EINVAL;
     if (!(R->scale > 0.0f) || R->scale > 3.4028234663852886e38f) return FLEXQ_EINVAL;
-    if ((long)M * R->k >= (1L << 31)) return FLEXQ_ESHAPE;
+    if ((long)M * R->k > kMostRows) return FLEXQ_ESHAPE;
     if (!aligned16(logits) || !aligned4(experts) || !aligned4(weights) || !aligned4(R->bias) || !aligned4(order) ||
         !aligned4(offsets))
         return FLEXQ_EALIGN;

@@ -134,6 +134,30 @@ def test_route_of_scores_closer_than_fp32_tells():
     check_route(logits, 8, score="sigmoid", groups=4, top_groups=2, group_top=2)
 
 
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("M,E,k", [(70, 8, 2), (33, 40, 15), (100, 256, 8), (20, 512, 16), (40, 64, 6), (9, 16, 16)])
+def test_route_of_pairs_that_fp32_cannot_tell_apart(M, E, k, score):
+    """Experts in pairs whose scores differ by less than fp32 scores are good to, in either order: few at a time (some
+    rows), or all (others); the last chosen and the first left out among them."""
+    rng = np.random.default_rng([M, E, k, 7])
+    logits = (1.5 * rng.standard_normal((M, E))).astype(np.float32)
+    for m in range(M):
+        pairs = rng.permutation(E).reshape(-1, 2)[:rng.integers(1, E // 2 + 1)]
+        up = rng.integers(0, 2, len(pairs)).astype(bool)
+        logits[m, pairs[:, 1]] = np.nextafter(logits[m, pairs[:, 0]], np.where(up, np.inf, -np.inf).astype(np.float32))
+    zero = np.zeros(E, np.float32)
+    check_route(logits, k, bias=zero, score=score)
+    check_route(logits, k, bias=zero, score=score, renormalise=False)
+    if E % 8 == 0:                                            # groups that repeat each other, a little higher or lower
+        size = E // 8
+        logits[:, size:2 * size] = np.nextafter(logits[:, :size], np.float32(np.inf))
+        logits[:, 5 * size:6 * size] = np.nextafter(logits[:, :size], np.float32(-np.inf))
+        for top_groups in (1, 4):
+            if k <= top_groups * size:
+                check_route(logits, k, bias=zero, score=score, groups=8, top_groups=top_groups, group_top=2)
+                check_route(logits, k, bias=zero, score=score, groups=8, top_groups=top_groups, group_top=1)
+
+
 # ---- the experts' linear layers ----------------------------------------------------------------------------------
 
 def draw_experts(rng, E, N, K, group):
@@ -424,3 +448,79 @@ def test_feed_forward_captured_and_on_another_stream():
             assert torch.equal(eager[name], kept[name]), (seed, name)
         for i in range(4):
             assert torch.equal(eager["route"][i], kept["route"][i]), (seed, i)
+
+
+# ---- limits and company ------------------------------------------------------------------------------------------
+
+def test_rows_past_32_bits():
+    """Outputs of more than 2^32 bytes: the last rows, through every kernel of the experts, the sum and the adapters."""
+    rng = np.random.default_rng(30)
+    E, N, K, slots = 2, 32768, 128, 70000
+    codes, sw = draw_experts(rng, E, N, K, 0)
+    xq, sx = draw_rows(rng, slots, K, 8)
+    ids = (np.arange(slots) % 2).astype(np.int32)
+    order, offsets = ref.group_rows(ids, E)
+    args = (fq.pack_experts(to_dev(codes), to_dev(sw)), N, K, to_dev(xq), to_dev(sx), to_dev(order), to_dev(offsets))
+    at = np.array([0, 34999, 35000, 65535, 65536, 69998, 69999])            # sorted rows
+    want, _ = ref.expert_rows(codes, sw, xq[order[at]], sx[order[at]], np.arange(at.size), np.array([0, 2, at.size]), 1, 0)
+    out = torch.empty((slots, N), dtype=torch.float16, device=DEV)
+    for form in (2, 3, 4, 5, 6):
+        say(f"form {form}")
+        out.fill_(7.0)
+        dev.expert_linear(form, *args, k=1, scatter=True, out=out)
+        assert_y_close(host(out[torch.from_numpy(order[at]).long().to(DEV)]), want.astype(np.float16))
+    M = slots // 2
+    experts = torch.zeros((M, 2), dtype=torch.int32, device=DEV)
+    weights = torch.rand((M, 2), dtype=torch.float32, device=DEV)
+    sums = fq.combine_experts(out, experts, weights)
+    rows = host(out[-6:])
+    want, bound = ref.combine(rows, np.zeros((3, 2), np.int32), host(weights[-3:]))
+    assert np.all(np.abs(host(sums[-3:]).astype(np.float64) - want) <= bound)
+    del sums
+    a, b, scale = draw_adapters(rng, 2, 16, K, N)
+    x = rng.standard_normal((slots, K)).astype(np.float16)
+    keep = host(out[-4:])
+    fq.adapters(to_dev(a), to_dev(b), to_dev(scale), to_dev(x), to_dev(order), to_dev(offsets), out, out=out)
+    want, bound = ref.adapters(a, b, scale, x[-4:], ids[-4:], keep)
+    assert np.all(np.abs(host(out[-4:]).astype(np.float64) - want) <= bound)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each call has a workspace of its own unless one is given: two streams' calls do not disturb each other."""
+    rng = np.random.default_rng(31)
+    runs = [FeedForward(90, 6, 2, 256, 256, 3, 16, 0, seed) for seed in (40, 41)]
+    alone = [f.run() for f in runs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in runs]
+    for _ in range(3):
+        both = []
+        for f, st in zip(runs, streams):
+            with torch.cuda.stream(st):
+                both.append(f.run())
+        torch.cuda.synchronize()
+        for one, two in zip(alone, both):
+            for name in ("out", "y", "z"):
+                assert torch.equal(one[name], two[name]), name
+
+
+def test_given_workspaces_and_refusals_on_the_device():
+    ids = torch.randint(-1, 5, (3000,), dtype=torch.int32, device=DEV)
+    ws = torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV)          # any content
+    for got, want in zip(fq.group_rows(ids, 5, workspace=ws), fq.group_rows(ids, 5)):
+        assert torch.equal(got, want)
+    logits = torch.randn((100, 16), device=DEV)
+    for got, want in zip(fq.route_experts(logits, 3, workspace=ws), fq.route_experts(logits, 3)):
+        assert torch.equal(got, want)
+    with pytest.raises(fq.FlexQError):
+        fq.group_rows(ids, 5, workspace=ws[:64])
+    with pytest.raises(fq.FlexQError):
+        fq.group_rows(ids, 5, workspace=torch.zeros(1 << 20))                # not on the device
+    with pytest.raises(fq.FlexQError):
+        fq.group_rows(ids[::2], 5)
+    with pytest.raises(fq.FlexQError):
+        fq.route_experts(logits, 17)
+    with pytest.raises(fq.FlexQError):
+        fq.route_experts(logits, 3, groups=5)
+    with pytest.raises(fq.FlexQError):
+        fq.route_experts(logits, 3, bias=torch.zeros(15, device=DEV))
+    assert fq.route_experts(logits, 3, group=False).order is None

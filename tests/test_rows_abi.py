@@ -29,7 +29,7 @@ def test_group_rows_refusals():
 
     for kw in (dict(ids=None), dict(order=None), dict(offsets=None), dict(rows=0), dict(rows=-1), dict(count=0)):
         assert call(**kw) == EINVAL, kw
-    assert call(count=513) == ESHAPE
+    assert call(count=513) == ESHAPE and call(rows=(1 << 28) + 1) == ESHAPE and size((1 << 28) + 1, 8) == 0
     for kw in (dict(ids=OFF), dict(order=OFF), dict(offsets=OFF), dict(ws=ODD)):
         assert call(**kw) == EALIGN, kw
     assert call(ws=None) == EWORKSPACE and call(wsb=size(2000, 8) - 1) == EWORKSPACE
@@ -59,7 +59,7 @@ def test_route_refusals():
     assert call(dict(k=17, groups=1, top_groups=1), E=64) == EINVAL
     assert call(dict(groups=128, top_groups=4), E=256) == EINVAL           # at most 64 groups
     assert call(dict(groups=1, top_groups=1), E=513) == ESHAPE
-    assert call(dict(groups=1, top_groups=1, k=16), E=64, M=1 << 27) == ESHAPE
+    assert call(dict(groups=1, top_groups=1, k=16), E=64, M=1 << 27) == ESHAPE and size(1 << 27, 64, 16) == 0
     for kw in (dict(logits=ODD), dict(experts=OFF), dict(weights=OFF), dict(order=OFF), dict(offsets=OFF), dict(ws=ODD)):
         assert call(**kw) == EALIGN, kw
     assert call(dict(bias=0x1002)) == EALIGN
@@ -112,6 +112,7 @@ def test_adapters_refusals():
     for kw in (dict(a=None), dict(b=None), dict(scale=None), dict(x=None), dict(order=None), dict(offsets=None), dict(y=None),
                dict(out=None), dict(L=0), dict(R=0), dict(M=0), dict(N=0), dict(K=0)):
         assert call(**kw) == EINVAL, kw
+    assert call(M=1 << 24, N=1 << 30) == ESHAPE                            # more workgroups than a launch has
     for kw in (dict(L=513), dict(R=8), dict(R=24), dict(R=272), dict(N=40), dict(K=200), dict(K=65536 + 128), dict(M=(1 << 24) + 1)):
         assert call(**kw) == ESHAPE, kw
     for kw in (dict(a=ODD), dict(b=ODD), dict(x=ODD), dict(y=ODD), dict(out=ODD), dict(scale=OFF), dict(order=OFF),
