@@ -284,15 +284,16 @@ int row_blocks(int M, int L, int R) { return R <= 128 && M >= 24 * (long)(L < M 
 long pieces_bound(int M, int groups, int height) { return M / height + (groups < M ? groups : M); }
 long pieces_likely(int M, int groups, int height) { return (M + height - 1) / height + (groups < M ? groups : M) / 2; }
 
-// K splits of the first launch: until there are about two workgroups a CU, but 1024 k (four steps a wavefront) or
-// more each, 512 where even then half the chip is idle (333 x 5248 of rank 32 17.3 -> 16.0 us).  Every split is a
-// share of h that the second launch's workgroups read: with 32-row pieces no more than 256 ranks' worth (rank 128
-// of 800 x 4096 in four 50 us, in two 31; rank 64 of 2048 x 8192 in eight 51, in four 46).
+// K splits of the first launch: until there are about two workgroups a CU -- one, of 32 rows at 64 ranks or more, whose
+// loads fill it (4096 x 4096 of rank 64 48 -> 43 us) -- but 1024 k (four steps a wavefront) or more each, 512 where
+// even then half the chip is idle (333 x 5248 of rank 32 17.3 -> 16.0 us).  Every split is a share of h that the
+// second launch's workgroups read: with 32-row pieces no more than 256 ranks' worth (rank 128 of 800 x 4096 in four
+// 50 us, in two 31; rank 64 of 2048 x 8192 in eight 51, in four 46).
 int splits_for(int M, int L, int R, int K)
 {
     const int blocks = row_blocks(M, L, R);
     const long pieces = pieces_likely(M, L, 16 * blocks);
-    long s = (512 + pieces - 1) / pieces;
+    long s = ((blocks == 2 && R >= 64 ? 256 : 512) + pieces - 1) / pieces;
     const int least = pieces * ((R + 63) / 64) * (K / 1024) <= 128 ? 512 : 1024;
     if (s > K / least) s = K / least;
     if (blocks == 2 && s > 256 / R) s = 256 / R;
