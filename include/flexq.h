@@ -14,6 +14,10 @@
  * quantized and packed once, offline; activations are quantized online
  * (Section 4.1.3, "FlexQ System Runtime").
  *
+ * Beside it, for batches whose rows choose their own weights: routing of tokens
+ * to experts, the experts' linear layers, low-rank adapters of many requests
+ * (at the end of this file).
+ *
  * Conventions for every entry point:
  *   - every pointer marked "dev" is DEVICE memory owned by the caller; the
  *     library allocates nothing and frees nothing;
@@ -410,8 +414,8 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *            slot s takes row s / k; k = 0: rows that are sorted already (x_rows = slots), as this call leaves them
  *   y        dev, out, fp16 [slots,N]: row r is that of slot order[r] (sorted rows), or with scatter = 1 row s
  *            is slot s.  Rows of slots without an expert are left as they were.  Must not overlap the inputs.
- * Same values as the dense call with that expert's weights, shapes and status codes as there; x_rows K and
- * 0.75 N K must be below 2^32.
+ * Same values as the dense call with that expert's weights (group-128 scales: but for the order of the fp32 sums),
+ * shapes and status codes as there; x_rows K and 0.75 N K must be below 2^32.
  * A feed-forward layer: flexq_route; flexq_quant_act or flexq_rmsnorm_quant of the tokens; gate|up with k and
  * scatter 0; flexq_swiglu_quant of all sorted rows (rows behind the last have any content); down with k = 0
  * and scatter = 1; flexq_expert_combine.

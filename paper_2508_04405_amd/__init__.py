@@ -1,4 +1,5 @@
-"""MI355X-native W6A6 / W6A8 quantized linear layer (GEMM + decode GEMV).
+"""MI355X-native W6A6 / W6A8 quantized linear layer (GEMM + decode GEMV), alone or by expert, with
+the routing to experts and the low-rank adapters of a batch's requests.
 
 `binding` is the thin ctypes layer over the C ABI in include/flexq.h; `synth`
 draws the seeded synthetic inputs; `build` compiles the HIP sources; `dev` (not

@@ -13,6 +13,13 @@
 // and lo = fp16(h - hi), which carry 22 bits (or 2^-38 of the row's largest), and both go through one
 // MFMA: its 32 k are 16 ranks of hi and the same 16 of lo, against B's 16 ranks twice.  The sum is
 // added to y in fp32 and rounded once.
+//
+// What bounds it: the low ranks' products are nothing (4096 rows of 4096 x 12288, rank 16: 2 GFLOP
+// beside 233 MB), so memory, in rows too short for a tile to be used twice: there the first launch
+// reads x at 2.3 TB/s, 14 us, the second reads y and writes out at 4.2, 48 us.  Few rows: the two
+// launches and their trips to memory, one after the other (one row 3.7 + 4.2 us, 333 rows of
+// 5248 x 13664 at rank 32 6.8 + 9.7).  64 ranks and more with many rows: the loads of A and B from L2,
+// which every 16 or 32 rows repeat (4096 x 4096 of rank 64 43 us at 105 MB).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"

@@ -1442,6 +1442,9 @@ __device__ __forceinline__ void run_items(const Args &a, uint8_t *lds, int &s_la
 
 // Rows grouped by expert: tiles of HIGH rows, then what is left of the experts as tiles of half of that (see
 // ExpertWalk).  How many there are is known here only.
+// Bound as the dense kernel by the power that the MFMAs take: 8 experts at 1024 rows, K 4096, N 22016 709 us, 2.1
+// POP/s, where one dense layer of as many rows takes 627 (the experts' last tiles are 6 % of rows that are not there);
+// group-128 scales by the vector unit (20 experts at 45 rows, K 2176, N 3424: 40 us from HBM, 31 from the caches).
 template <int GROUP>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void gemm_expert_kernel(flexq::ExpertLinear a, int tiles_n)
