@@ -87,6 +87,21 @@ def test_route_groups_and_bias(M, E, k, groups, top_groups, group_top, score):
         check_route(logits, k, bias=b, score=score, groups=groups, top_groups=top_groups, group_top=group_top, renormalise=False)
 
 
+@pytest.mark.parametrize("M,E,k,groups,top_groups", [(40, 16, 3, 2, 1), (50, 100, 5, 4, 2), (70, 256, 8, 8, 4), (21, 510, 16, 17, 6)])
+def test_route_of_fp16_logits_with_bias_and_groups(M, E, k, groups, top_groups):
+    """Logits of 16 bits: scores that are equal without the bias are the rule."""
+    say(f"route fp16 M={M} E={E} k={k} groups={groups}/{top_groups}")
+    rng = np.random.default_rng([M, E, 16])
+    logits = rng.standard_normal((M, E)).astype(np.float16)
+    logits[:, ::3] = np.float16(0.5)
+    bias = (0.1 * rng.standard_normal(E)).astype(np.float32)
+    bias[: E // 2] = 0.25
+    for score in ("softmax", "sigmoid"):
+        check_route(logits, k, bias=bias, score=score)
+        check_route(logits, k, bias=bias, score=score, groups=groups, top_groups=top_groups, group_top=2)
+        check_route(logits, k, score=score, groups=groups, top_groups=top_groups, group_top=2, renormalise=False)
+
+
 @pytest.mark.parametrize("kw", [dict(score="softmax"), dict(score="sigmoid", renormalise=False),
                                 dict(score="sigmoid", groups=8, top_groups=3, group_top=2),
                                 dict(score="softmax", groups=8, top_groups=2, group_top=1)])
@@ -316,6 +331,15 @@ def test_adapters_of_a_long_row():
     a, b, scale = draw_adapters(rng, 2, 32, 28672, 96)
     x = rng.standard_normal((5, 28672)).astype(np.float16)
     check_adapters(a, b, scale, x, np.array([0, 1, -1, 0, 1], np.int32), rng.standard_normal((5, 96)).astype(np.float16))
+
+
+@pytest.mark.parametrize("R", [16, 48, 64, 128])
+def test_adapters_of_many_rows_and_a_long_row(R):
+    """Pieces of 32 rows, K split over workgroups."""
+    rng = np.random.default_rng([15, R])
+    a, b, scale = draw_adapters(rng, 2, R, 8192, 96)
+    ids = rng.integers(-1, 2, 100).astype(np.int32)
+    check_adapters(a, b, scale, rng.standard_normal((100, 8192)).astype(np.float16), ids, rng.standard_normal((100, 96)).astype(np.float16))
 
 
 def test_adapters_keep_small_and_large_rows_apart():
