@@ -18,7 +18,7 @@
 // beside 233 MB), so memory, in rows too short for a tile to be used twice: there the first launch
 // reads x at 2.3 TB/s, 14 us, the second reads y and writes out at 4.2, 48 us.  Few rows: the two
 // launches and their trips to memory, one after the other (one row 3.7 + 4.2 us, 333 rows of
-// 5248 x 13664 at rank 32 6.8 + 9.7).  64 ranks and more with many rows: the loads of A and B from L2,
+// 5248 x 13664 at rank 32 5.7 + 9.4).  64 ranks and more with many rows: the loads of A and B from L2,
 // which every 16 or 32 rows repeat (4096 x 4096 of rank 64 43 us at 105 MB).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
@@ -200,17 +200,37 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs p, int rest
         for (int k = 0; k < RB; ++k)
 #pragma unroll
             for (int t = 0; t < RT; ++t) v[k][t] = 0.0f;
-        // (all of a split's shares set out together: one after the other they are most of a small call)
+        // (four splits' shares set out together: one after the other they are most of a small call.  More than sixteen
+        // loads the compiler does not gather by itself: rank 128 of 64 x 4096 20.8 us, 12.4 with the array)
+        auto share = [&](int s, int k, int t) {
+            const int m = min(16 * k + (tid >> 4), rows - 1);         // (rows beyond the last repeat it and are not stored)
+            return t < live ? p.h[((size_t)s * p.M + first + m) * p.R + 16 * t + q] : 0.0f;
+        };
+        if constexpr (RT * RB <= 4) {
 #pragma unroll 4
-        for (int s = 0; s < p.splits; ++s)
+            for (int s = 0; s < p.splits; ++s)
 #pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                const int m = min(16 * k + (tid >> 4), rows - 1);     // (rows beyond the last repeat it and are not stored)
-                const float *from = p.h + ((size_t)s * p.M + first + m) * p.R + q;
+                for (int k = 0; k < RB; ++k)
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
-                    if (t < live) v[k][t] += from[16 * t];
+                    for (int t = 0; t < RT; ++t) v[k][t] += share(s, k, t);
+        } else {
+            for (int s = 0; s < p.splits; s += 4) {
+                float w[4][RB][RT];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int k = 0; k < RB; ++k)
+#pragma unroll
+                        for (int t = 0; t < RT; ++t) w[u][k][t] = share(min(s + u, p.splits - 1), k, t);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (s + u < p.splits)
+#pragma unroll
+                        for (int k = 0; k < RB; ++k)
+#pragma unroll
+                            for (int t = 0; t < RT; ++t) v[k][t] += w[u][k][t];
             }
+        }
 #pragma unroll
         for (int k = 0; k < RB; ++k) {
             const int m = 16 * k + (tid >> 4);
@@ -283,27 +303,37 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs p, int rest
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Rows of a piece, by 16: two where an adapter has 24 rows or more on average -- A and B, from L2, then feed twice
-// the rows.
-int row_blocks(int M, int L, int R) { return R <= 128 && M >= 24 * (long)(L < M ? L : M) ? 2 : 1; }
-
 // Pieces that M rows of `groups` groups can come in, and about how many they will be.
 long pieces_bound(int M, int groups, int height) { return M / height + (groups < M ? groups : M); }
 long pieces_likely(int M, int groups, int height) { return (M + height - 1) / height + (groups < M ? groups : M) / 2; }
 
+// Rows of a piece, by 16, of either launch (they may differ, h lies by place).  Two read A or B, from L2, half as often,
+// but begin dearer and are fewer: they pay where adapters have 24 rows or more on average, in the first launch from
+// about 5 million values of x on, whatever the rank, in the second where sixteen rows a piece would read 50 MB of B.  us
+// with one / two in both launches: 64 x 4096 x 4096 of rank 64 10.4 / 13.0, 200 x 12288 x 4096 of rank 32 11 / 14, 2000 x
+// 4096 x 4096 of rank 64 29.3 / 25.2, 2000 x 8192 x 28672 of rank 128 192 / 132.  (Over 208 shapes of 26 .. 4096 rows
+// this takes 1.01 times the best of the four combinations' time on average, two from 24 rows on 1.11.)
+int row_blocks(int M, int L, int R, bool enough)
+{
+    return R <= 128 && M >= 24 * (long)(L < M ? L : M) && enough ? 2 : 1;
+}
+int down_blocks(int M, int L, int R, int K) { return row_blocks(M, L, R, pieces_likely(M, L, 16) * K >= 300000); }
+int up_blocks(int M, int L, int R, int N) { return row_blocks(M, L, R, pieces_likely(M, L, 16) * R * N >= 25000000); }
+
 // K splits of the first launch: until there are about two workgroups a CU -- one, of 32 rows at 64 ranks or more, whose
 // loads fill it (4096 x 4096 of rank 64 48 -> 43 us) -- but 1024 k (four steps a wavefront) or more each, 512 where
 // even then half the chip is idle (333 x 5248 of rank 32 17.3 -> 16.0 us).  Every split is a share of h that the
-// second launch's workgroups read: with 32-row pieces no more than 256 ranks' worth (rank 128 of 800 x 4096 in four
-// 50 us, in two 31; rank 64 of 2048 x 8192 in eight 51, in four 46).
+// second launch's workgroups read, four at a time: with 32-row pieces no more than 512 ranks' worth (rank 128 of 600 x
+// 12288 x 4096 in two 47 us, in four 33, in eight 35), and above four a multiple of four.
 int splits_for(int M, int L, int R, int K)
 {
-    const int blocks = row_blocks(M, L, R);
+    const int blocks = down_blocks(M, L, R, K);
     const long pieces = pieces_likely(M, L, 16 * blocks);
     long s = ((blocks == 2 && R >= 64 ? 256 : 512) + pieces - 1) / pieces;
     const int least = pieces * ((R + 63) / 64) * (K / 1024) <= 128 ? 512 : 1024;
     if (s > K / least) s = K / least;
-    if (blocks == 2 && s > 256 / R) s = 256 / R;
+    if (blocks == 2 && s > 512 / R) s = 512 / R;
+    if (s > 4) s -= s % 4;
     return s < 1 ? 1 : s > 64 ? 64 : (int)s;
 }
 
@@ -369,14 +399,14 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
     p.N = N;
     p.K = K;
     p.splits = splits_for(M, L, R, K);
-    const int blocks = row_blocks(M, L, R), height = 16 * blocks, tiles = R / 16;
+    const int tiles = R / 16, down_by = down_blocks(M, L, R, K), up_by = up_blocks(M, L, R, N);
     // the rows without an adapter need no products, and nothing at all where out is y
     const int rest = out != y ? 1 : 0;
-    p.columns = up_columns(pieces_likely(M, L + rest, height), N, tiles, blocks);
+    p.columns = up_columns(pieces_likely(M, L + rest, 16 * up_by), N, tiles, up_by);
     hipStream_t st = (hipStream_t)stream;
     const int rt = tiles == 1 ? 1 : tiles == 2 ? 2 : 4, chunks = (tiles + rt - 1) / rt;
-    const long down_grid = pieces_bound(M, L, height) * chunks * p.splits;
-    const long up_grid = pieces_bound(M, L + rest, height) * ((N + p.columns - 1) / p.columns);
+    const long down_grid = pieces_bound(M, L, 16 * down_by) * chunks * p.splits;
+    const long up_grid = pieces_bound(M, L + rest, 16 * up_by) * ((N + p.columns - 1) / p.columns);
     if (down_grid >= (1L << 31) || up_grid >= (1L << 31)) return FLEXQ_ESHAPE;
     auto down = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)down_grid), dim3(256), 0, st, p, chunks);
@@ -387,7 +417,7 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
         return hipGetLastError();
     };
     hipError_t e;
-    if (blocks == 2)
+    if (down_by == 2)
         e = rt == 1          ? down(adapter_down_kernel<1, 2, 4, true>)
             : rt == 2        ? down(adapter_down_kernel<2, 2, 2, true>)
             : tiles % 4 == 0 ? down(adapter_down_kernel<4, 2, 2, true>)
@@ -398,7 +428,7 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
             : tiles % 4 == 0 ? down(adapter_down_kernel<4, 1, 2, true>)
                              : down(adapter_down_kernel<4, 1, 2, false>);
     if (e != hipSuccess) return FLEXQ_EHIP;
-    if (blocks == 2)
+    if (up_by == 2)
         switch (tiles) {
         case 1: e = up(adapter_up_kernel<0, 2, true>); break;
         case 2: e = up(adapter_up_kernel<1, 2, true>); break;

@@ -342,6 +342,16 @@ def test_adapters_of_many_rows_and_a_long_row(R):
     check_adapters(a, b, scale, rng.standard_normal((100, 8192)).astype(np.float16), ids, rng.standard_normal((100, 96)).astype(np.float16))
 
 
+@pytest.mark.parametrize("R,N", [(16, 20608), (32, 10304), (48, 6912), (64, 5152), (80, 4128), (112, 2976), (128, 2592)])
+def test_adapters_in_pieces_of_32_rows(R, N):
+    """So many rows that both launches take them 32 at a time."""
+    rng = np.random.default_rng([16, R])
+    a, b, scale = draw_adapters(rng, 2, R, 4096, N)
+    ids = np.concatenate([np.zeros(37, np.int32), np.ones(1123, np.int32), np.full(40, -1, np.int32)])
+    rng.shuffle(ids)
+    check_adapters(a, b, scale, rng.standard_normal((1200, 4096)).astype(np.float16), ids, rng.standard_normal((1200, N)).astype(np.float16))
+
+
 def test_adapters_keep_small_and_large_rows_apart():
     """The intermediate keeps 32 bits: rows whose A x lies outside fp16's range on either side, next to ordinary ones; a
     row that is not finite stays by itself."""
