@@ -225,12 +225,13 @@ __device__ __forceinline__ bool near(unsigned above, unsigned below)
     return !(x - y > kClose * fmaxf(1.0f, fmaxf(fabsf(x), fabsf(y))));
 }
 
-// Keeps the keys of the top_groups best groups.  key_of_pair: the key of a group from its best two; unsure: set
-// where the first group left out is `close` to the last one kept.  G: groups a lane of the row keeps (1: up to 16
-// groups, each scanned by as many lanes as there are for it).
-template <int V, int G, class Pair, class Close>
-__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane,
-                                            const Pair &key_of_pair, const Close &close, bool &unsure)
+// Keeps the keys of the top_groups best groups.  unsure: set where fp32 does not tell a group left out from one kept: c
+// is off by 2^-21 of its size, at least of 1 -- its own, not that of a sum in which two large ones cancel -- so half a
+// group's worth lies within 1.5 2^-21 of the larger of the c in it (both of them, and the rounding of the sum and of the
+// interval's ends; halves do not overflow).  G: groups a lane of the row keeps (1: up to 16 groups, each scanned by
+// as many lanes as there are for it).
+template <bool BY_LOGIT, int V, int G>
+__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane, bool &unsure)
 {
     const int l = lane & 15;
 #pragma unroll
@@ -238,7 +239,9 @@ __device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[
         if (l * V + v < a.E) scratch[padded(l * V + v)] = key[v];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (a wavefront's own part of LDS: no barrier)
     const int shift = G == 1 ? a.group_shift : 0, P = 1 << shift;     // P lanes a group
+    const bool pair = !BY_LOGIT && a.group_top == 2;
     unsigned of_group[G];
+    float half[G], off[G];                                   // (off < 0: there is none)
 #pragma unroll
     for (int q = 0; q < G; ++q) {
         const int g = G == 1 ? l >> shift : l * G + q;
@@ -255,18 +258,32 @@ __device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[
                 second = max(max(second, s), min(first, f));
                 first = max(first, f);
             }
-        of_group[q] = (l & (P - 1)) == 0 && first != 0 ? key_of_pair(first, second) : 0u;
+        const float x = value_of(first), y = pair && second != 0 ? value_of(second) : 0.0f;
+        of_group[q] = (l & (P - 1)) != 0 || first == 0 ? 0u : pair && second != 0 ? key_of(x + y) : first;
+        half[q] = 0.5f * x + 0.5f * y;
+        off[q] = first != 0 ? 0.75f * kClose * fmaxf(1.0f, fmaxf(fabsf(x), fabsf(y))) : -1.0f;
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read before the next tokens' keys come)
     unsigned long long kept = 0;
-    unsigned last = 0, next;
+    unsigned wins;
     for (int i = 0; i < a.top_groups; ++i) {
-        const int g = pick(of_group, lane, next);
+        const int g = pick(of_group, lane, wins);
         if (g >= 0) kept |= 1ull << (g >> shift);
-        last = next;
     }
-    pick(of_group, lane, next);
-    if (last != 0 && next != 0 && close(last, next)) unsure = true;
+    if constexpr (!BY_LOGIT) {
+        float low = INFINITY, high = -INFINITY;              // the least that a kept one may be, the most another may
+#pragma unroll
+        for (int q = 0; q < G; ++q)
+            if (off[q] >= 0.0f) {
+                if ((kept >> (G == 1 ? l >> shift : l * G + q)) & 1)
+                    low = fminf(low, half[q] - off[q]);
+                else
+                    high = fmaxf(high, half[q] + off[q]);
+            }
+        low = row_all_f(low, [](float p, float q) { return fminf(p, q); });
+        high = row_all_f(high, [](float p, float q) { return fmaxf(p, q); });
+        unsure |= !(low > high);
+    }
     if ((a.group_size & (V - 1)) == 0) {                     // a lane's experts are of one group
         const unsigned of = (unsigned)(((unsigned)(l * V) * a.group_inv) >> 32);
         const bool in = (kept >> (of & 63)) & 1;
@@ -280,14 +297,13 @@ __device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[
         }
     }
 }
-template <int V, class Pair, class Close>
-__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane,
-                                            const Pair &key_of_pair, const Close &close, bool &unsure)
+template <bool BY_LOGIT, int V>
+__device__ __forceinline__ void keep_groups(const RouteArgs &a, unsigned (&key)[V], unsigned *scratch, int lane, bool &unsure)
 {
     if (a.groups <= 16)
-        keep_groups<V, 1>(a, key, scratch, lane, key_of_pair, close, unsure);
+        keep_groups<BY_LOGIT, V, 1>(a, key, scratch, lane, unsure);
     else
-        keep_groups<V, 4>(a, key, scratch, lane, key_of_pair, close, unsure);
+        keep_groups<BY_LOGIT, V, 4>(a, key, scratch, lane, unsure);
 }
 
 // The best of a whole wavefront's 64-bit keys, as pick() above: its index l V + v for lane l.
@@ -502,15 +518,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
             for (int v = 0; v < V; ++v) key[v] = x[v] > -INFINITY && c[v] > -INFINITY ? key_of(c[v]) : 0u;
         }
         bool unsure = false;                                 // all the experts have to be looked at in 64 bits
-        if (a.top_groups < a.groups)
-            keep_groups(a, key, scratch, lane,
-                        [&](unsigned f, unsigned s) {
-                            return !BY_LOGIT && a.group_top == 2 && s != 0 ? key_of(value_of(f) + value_of(s)) : f;
-                        },
-                        [](unsigned p, unsigned q) {         // (sums of two: twice as far)
-                            return !BY_LOGIT && near(key_of(0.5f * value_of(p)), key_of(0.5f * value_of(q)));
-                        },
-                        unsure);
+        if (a.top_groups < a.groups) keep_groups<BY_LOGIT>(a, key, scratch, lane, unsure);
         int mine = -1;                                       // the expert of slot l
         unsigned last = 0, wins = 0;
         bool close = false;                                  // two that follow each other are
