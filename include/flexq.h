@@ -403,7 +403,8 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *   workspace       as for flexq_group_rows, flexq_route_workspace_bytes(M, E, k); may be NULL without order
  *                   and for up to 32 tokens
  * The choice is that of c in 64 bits where a bias or a sum enters it, and of the logits themselves where none does;
- * weights are good to a few ulp of fp32, also where the scores themselves underflow (sigmoids far below zero).
+ * weights are good to 18 * 2^-24 of themselves (a softmax without renormalise 24 * 2^-24), or where they are subnormal to a
+ * few steps of 2^-149, scale times; renormalised ones also where the scores themselves underflow.
  * 1 <= k <= FLEXQ_MAX_EXPERTS_PER_TOKEN, k <= top_groups * E / groups, groups <= 64, 0 < scale < inf.
  *
  * flexq_expert_linear: the linear layer (flexq_gemm_w6a6 / _w6a8, codes of either width) of E experts on

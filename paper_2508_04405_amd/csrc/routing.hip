@@ -413,6 +413,16 @@ __device__ __forceinline__ int order_exactly(const RouteArgs &a, float lv, int m
     return __builtin_amdgcn_ds_permute(4 * ((lane & 48) | rank), mine);
 }
 
+// e^(x - y), y no less than x, both finite: what the difference lost in rounding, up to 2^-24 of it and so many times
+// that of the result, is exact in fp32 and put right to first order.
+__device__ __forceinline__ float exp_of_difference(float x, float y)
+{
+    const float d = x - y, back = d - x;
+    const float lost = (x - (d - back)) - (y + back);
+    const float e = expf(d);
+    return d > -110.0f ? __builtin_fmaf(e, lost, e) : 0.0f;      // (e^-104 is less than any fp32)
+}
+
 // BY_LOGIT: the logits are compared; else c.
 template <bool BY_LOGIT, int V, bool HALF>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
@@ -484,10 +494,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
         if (!a.sigmoid && (!BY_LOGIT || !a.renormalise)) {
             top = row_all_f(top, [](float p, float q) { return fmaxf(p, q); });
             if constexpr (BY_LOGIT) {
-                float sum = 0.0f;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};     // (a sum of 32 by itself would be off by 31 roundings)
 #pragma unroll
-                for (int v = 0; v < V; ++v) sum += x[v] > -INFINITY ? expf(x[v] - top) : 0.0f;
-                total = row_all_f(sum, [](float p, float q) { return p + q; });
+                for (int v = 0; v < V; ++v) sum[v & 3] += x[v] > -INFINITY ? expf(x[v] - top) : 0.0f;
+                total = row_all_f((sum[0] + sum[1]) + (sum[2] + sum[3]), [](float p, float q) { return p + q; });
             } else {                     // in 64 bits: the roundings of 512 additions would be more than c may be off by
                 double sum = 0.0;
 #pragma unroll
@@ -569,18 +579,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a)
             }
         }
 
-        // weights: softmax renormalised from the largest of the chosen, so that nothing underflows; sigmoids that
-        // all lie far below 0 are exponentials there
+        // weights: renormalised from the largest of the chosen, so that nothing underflows which is not small beside it
+        // (sigmoids of negative logits are e^l / (1 + e^l))
         const bool chosen = l < k && mine >= 0;
         float lv = -INFINITY;
         if (chosen) lv = fminf(HALF ? h2f(half[mine]) : full[mine], kLargest);
         const float above = row_all_f(lv, [](float p, float q) { return fmaxf(p, q); });
         float w = 0.0f;
         if (chosen) {
-            if (a.renormalise && (!a.sigmoid || above < -60.0f))
-                w = expf(lv - above);
-            else
-                w = a.sigmoid ? 1.0f / (1.0f + expf(-lv)) : expf(lv - top) / total;
+            if (!a.sigmoid) {
+                w = a.renormalise ? exp_of_difference(lv, above) : exp_of_difference(lv, top) / total;
+            } else if (a.renormalise && above < 0.0f) {
+                w = exp_of_difference(lv, above) / (1.0f + expf(lv));
+            } else {
+                const float t = expf(-fabsf(lv));
+                w = (lv < 0.0f ? t : 1.0f) / (1.0f + t);
+            }
         }
         if (a.renormalise) {
             const float sum = row_all_f(w, [](float p, float q) { return p + q; });
