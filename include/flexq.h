@@ -433,7 +433,8 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *   x, y     dev, fp16 [M,K] (the projection's input) and [M,N];  out  dev, fp16 [M,N], may be y
  *   order, offsets   the grouping of the M rows over the L adapters
  *   workspace   flexq_adapters_workspace_bytes(M, L, R, K) bytes, 16-byte aligned, any content
- * fp32 sums in a fixed order, the intermediate A x to 2^-22 of itself (2^-38 of the row's largest), one rounding.
+ * Sums are fp32 in a fixed order; the sum A x then enters the second product with 22 bits of itself (what is below
+ * 2^-38 of the row's largest is lost); one rounding at the end.
  * K % 128 == 0, K <= FLEXQ_MAX_K, N % 32 == 0, M <= 2^24.
  */
 #define FLEXQ_MAX_EXPERTS 512
