@@ -427,14 +427,15 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *
  * flexq_adapters: low-rank adapters beside a projection y that all rows of a batch share,
  *   out[m] = fp16( y[m] + scale[l] * B_l (A_l x[m]) ),   l the adapter of row m; out[m] = y[m] without one.
- *   a, b     dev, fp16 [L,R,K] and [L,N,R], 16-byte aligned: the L adapters, R (a multiple of 16, at most
- *            FLEXQ_MAX_RANK) the largest rank, shorter ones padded with zero rows of A (and finite values of B)
+ *   a, b     dev, fp16 [L,R,K] and [L,N,R], 16-byte aligned, finite: the L adapters, R (a multiple of 16, at
+ *            most FLEXQ_MAX_RANK) the largest rank, shorter ones padded with zero rows of A (and any values of B)
  *   scale    dev, fp32 [L], finite
  *   x, y     dev, fp16 [M,K] (the projection's input) and [M,N];  out  dev, fp16 [M,N], may be y
  *   order, offsets   the grouping of the M rows over the L adapters
  *   workspace   flexq_adapters_workspace_bytes(M, L, R, K) bytes, 16-byte aligned, any content
  * Sums are fp32 in a fixed order; the sum A x then enters the second product with 22 bits of itself (what is below
- * 2^-38 of the row's largest is lost); one rounding at the end.
+ * 2^-38 of the row's largest is lost); one rounding at the end.  Infinities and NaN of a row of x or y stay in that
+ * row, as fp32 arithmetic has them (0 times infinity is NaN: an adapter padded with zero rows gives NaN there).
  * K % 128 == 0, K <= FLEXQ_MAX_K, N % 32 == 0, M <= 2^24.
  */
 #define FLEXQ_MAX_EXPERTS 512

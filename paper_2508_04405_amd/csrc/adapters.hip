@@ -239,14 +239,17 @@ __global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs p, int rest
             for (int t = 0; t < RT; ++t) top = fmaxf(top, fabsf(v[k][t]));
 #pragma unroll
             for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+            // an infinite row is what its infinite ranks make of it: the others, finite, stay so, and nothing is taken
+            // from an infinity
+            const bool infinite = top == INFINITY;
             int e = 0;
-            if (top > 0.0f) e = 14 - (__builtin_amdgcn_frexp_expf(top));
+            if (top > 0.0f) e = infinite ? -60 : 14 - (__builtin_amdgcn_frexp_expf(top));
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 const float w = __builtin_amdgcn_ldexpf(v[k][t], e);
                 const _Float16 hi = (_Float16)w;
                 h[0][m][16 * t + q] = hi;
-                h[1][m][16 * t + q] = (_Float16)(w - (float)hi);
+                h[1][m][16 * t + q] = infinite ? (_Float16)0.0f : (_Float16)(w - (float)hi);
             }
             if (q == 0) back[m] = __builtin_amdgcn_ldexpf(p.scale[g.id], -e);
         }
