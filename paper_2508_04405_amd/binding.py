@@ -458,6 +458,13 @@ def _here(t, dtype, shape, dev):
     return t
 
 
+def _sizes(t, names):
+    """The sizes of a tensor that has one for each name."""
+    if t.dim() != len(names):
+        raise FlexQError(f"flexq: expected a tensor [{', '.join(names)}], got {list(t.shape)}")
+    return t.shape
+
+
 def _scratch(nbytes, given, device, cur):
     if nbytes == 0:
         raise FlexQError("flexq: invalid shape for workspace")
@@ -514,8 +521,14 @@ def route_experts(logits, k, score="softmax", bias=None, groups=1, top_groups=1,
 
 def pack_experts(wq, sw, group=0):
     """int8 codes [E,N,K] and fp16 scales [E,N] or [E,N,K/128] -> uint8 [E, packed_bytes(N, K, group)]."""
-    E, N, K = wq.shape
-    packed = torch.empty((E, packed_bytes(N, K, group)), dtype=torch.uint8, device=wq.device)
+    E, N, K = _sizes(wq, ("E", "N", "K"))
+    nbytes = packed_bytes(N, K, group)
+    if E < 1 or nbytes == 0:
+        raise FlexQError("flexq: invalid shape or group of the experts' weights")
+    cur = _current(wq)
+    _here(wq, torch.int8, (E, N, K), cur)
+    _here(sw, torch.float16, (E, N) if group == 0 else (E, N, K // 128), cur)
+    packed = torch.empty((E, nbytes), dtype=torch.uint8, device=wq.device)
     for e in range(E):
         packed[e] = pack_w6(wq[e], sw[e], group)
     return packed
