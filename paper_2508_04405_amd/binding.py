@@ -435,6 +435,7 @@ def layer_linears(layer, M, workspace, first_stage=0, last_stage=3, **buffers):
 Routing = collections.namedtuple("Routing", "experts weights order offsets")
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _ROUTE_ONE_LAUNCH = 32                  # tokens that flexq_route groups without a workspace
+_MOST_PER_TOKEN = 16                    # FLEXQ_MAX_EXPERTS_PER_TOKEN
 
 
 def _current(t):
@@ -499,6 +500,8 @@ def route_experts(logits, k, score="softmax", bias=None, groups=1, top_groups=1,
     dtype = logits.dtype
     if (dtype != torch.float32 and dtype != torch.float16) or logits.dim() != 2:
         raise FlexQError(f"flexq: logits are fp32 or fp16 [M, E], got {dtype} {list(logits.shape)}")
+    if not 0 < k <= _MOST_PER_TOKEN:     # (ahead of the outputs, which take memory by it)
+        raise FlexQError(f"flexq: 1 to {_MOST_PER_TOKEN} experts a token, got {k}")
     M, E = logits.shape
     cur = _current(logits)
     _here(logits, dtype, (M, E), cur)
@@ -542,7 +545,8 @@ def expert_linear(packed, N, K, xq, sx, order, offsets, group=0, k=0, scatter=Fa
     nbytes = lib.flexq_packed_bytes(N, K, group)
     if nbytes == 0:
         raise FlexQError("flexq: invalid shape or group of the experts' weights")
-    E, slots, rows, cur = packed.shape[0], order.numel(), xq.shape[0], _current(xq)
+    E, rows = _sizes(packed, ("E", "bytes"))[0], _sizes(xq, ("rows", "K"))[0]
+    slots, cur = order.numel(), _current(xq)
     _here(packed, torch.uint8, (E, nbytes), cur)
     _here(xq, torch.int8, (rows, K), cur)
     _here(sx, torch.float16, (rows,), cur)
@@ -558,8 +562,8 @@ def combine_experts(y, experts, weights, add=None, out=None):
     """The weighted sum over each token's slots: fp16 y [M * k, N] by slot, experts int32 and weights fp32 [M,k],
     plus fp16 add [M,N] if given -> fp16 [M,N].  Slots with a negative expert are left out."""
     lib = load()
-    M, k = experts.shape
-    N, cur = y.shape[1], _current(y)
+    M, k = _sizes(experts, ("M", "k"))
+    N, cur = _sizes(y, ("M * k", "N"))[1], _current(y)
     _here(y, torch.float16, (M * k, N), cur)
     _here(experts, torch.int32, (M, k), cur)
     _here(weights, torch.float32, (M, k), cur)
@@ -576,8 +580,8 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
     x fp16 [M,K], y fp16 [M,N], (order, offsets) from group_rows(ids, L); rows without an adapter keep y.
     `out` may be y."""
     lib = load()
-    L, R, K = a.shape
-    M, N = y.shape
+    L, R, K = _sizes(a, ("L", "R", "K"))
+    M, N = _sizes(y, ("M", "N"))
     cur, half, i32 = _current(x), torch.float16, torch.int32
     _here(a, half, (L, R, K), cur)
     _here(b, half, (L, N, R), cur)
