@@ -423,7 +423,7 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *
  * flexq_expert_combine: out[m] = fp16( add[m] + sum_j weights[m][j] * y[m k + j] ), in fp32, j ascending, over
  * the slots whose expert is not negative; y fp16 [M k,N], add fp16 [M,N] or NULL (a shared expert's output, the
- * residual; may be out), out fp16 [M,N]; N a multiple of 32.
+ * residual; may be out), out fp16 [M,N]; N a multiple of 32, M N <= 2^35 - 2048.
  *
  * flexq_adapters: low-rank adapters beside a projection y that all rows of a batch share,
  *   out[m] = fp16( y[m] + scale[l] * B_l (A_l x[m]) ),   l the adapter of row m; out[m] = y[m] without one.

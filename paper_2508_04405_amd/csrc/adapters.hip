@@ -410,7 +410,7 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
     const int rt = tiles == 1 ? 1 : tiles == 2 ? 2 : 4, chunks = (tiles + rt - 1) / rt;
     const long down_grid = pieces_bound(M, L, 16 * down_by) * chunks * p.splits;
     const long up_grid = pieces_bound(M, L + rest, 16 * up_by) * ((N + p.columns - 1) / p.columns);
-    if (down_grid >= (1L << 31) || up_grid >= (1L << 31)) return FLEXQ_ESHAPE;
+    if (down_grid >= (1L << 24) || up_grid >= (1L << 24)) return FLEXQ_ESHAPE;      // 256 threads each, 2^32 a launch
     auto down = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)down_grid), dim3(256), 0, st, p, chunks);
         return hipGetLastError();

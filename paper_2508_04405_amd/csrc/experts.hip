@@ -339,7 +339,7 @@ flexq_status flexq_expert_combine(const uint16_t *y, const int32_t *experts, con
                                   int M, int k, int N, uint16_t *out, void *stream)
 {
     if (!y || !experts || !weights || !out || M < 1 || N < 1 || k < 1 || k > FLEXQ_MAX_EXPERTS_PER_TOKEN) return FLEXQ_EINVAL;
-    if (N % 32 != 0 || (long)M * N / 8 >= (1L << 31) * 256) return FLEXQ_ESHAPE;
+    if (N % 32 != 0 || (long)M * N / 8 > (1L << 32) - 256) return FLEXQ_ESHAPE;     // (threads of a launch)
     if (!aligned16(y) || !aligned16(out) || (add && !aligned16(add)) || !aligned4(experts) || !aligned4(weights))
         return FLEXQ_EALIGN;
     const unsigned blocks = (unsigned)(((long)M * (N / 8) + 255) / 256);
