@@ -415,8 +415,10 @@ flexq_status flexq_gemv_w6a8_noalloc(const void *packed, int group, const int8_t
  *            slot s takes row s / k; k = 0: rows that are sorted already (x_rows = slots), as this call leaves them
  *   y        dev, out, fp16 [slots,N]: row r is that of slot order[r] (sorted rows), or with scatter = 1 row s
  *            is slot s.  Rows of slots without an expert are left as they were.  Must not overlap the inputs.
- * Same values as the dense call with that expert's weights (group-128 scales: but for the order of the fp32 sums),
- * shapes and status codes as there; x_rows K and 0.75 N K must be below 2^32.
+ * The dense call's values with that expert's weights, y = fp16( float(acc) * (sx * sw) ), the sum exact; kernels for few
+ * rows round the product to fp16 at once and tiles to fp32 before, here as in the dense call, so that outputs of two kernels
+ * may differ by an ulp of fp16 (about one in 17000 does).  Group-128 scales: sums in fp32, in an order of the kernel's own.
+ * Shapes and status codes as there; x_rows K and 0.75 N K must be below 2^32.
  * A feed-forward layer: flexq_route; flexq_quant_act or flexq_rmsnorm_quant of the tokens; gate|up with k and
  * scatter 0; flexq_swiglu_quant of all sorted rows (rows behind the last have any content); down with k = 0
  * and scatter = 1; flexq_expert_combine.
