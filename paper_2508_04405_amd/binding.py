@@ -526,14 +526,12 @@ def pack_experts(wq, sw, group=0):
     """int8 codes [E,N,K] and fp16 scales [E,N] or [E,N,K/128] -> uint8 [E, packed_bytes(N, K, group)]."""
     E, N, K = _sizes(wq, ("E", "N", "K"))
     nbytes = packed_bytes(N, K, group)
-    if E < 1 or nbytes == 0:
+    if E < 1 or nbytes == 0 or sw.dim() < 1 or sw.shape[0] != E:
         raise FlexQError("flexq: invalid shape or group of the experts' weights")
-    cur = _current(wq)
-    _here(wq, torch.int8, (E, N, K), cur)
-    _here(sw, torch.float16, (E, N) if group == 0 else (E, N, K // 128), cur)
+    cur, scales = _current(wq), (N,) if group == 0 else (N, K // 128)
     packed = torch.empty((E, nbytes), dtype=torch.uint8, device=wq.device)
-    for e in range(E):
-        packed[e] = pack_w6(wq[e], sw[e], group)
+    for e in range(E):                    # (each expert's own are contiguous, all of them need not be)
+        packed[e] = pack_w6(_here(wq[e], torch.int8, (N, K), cur), _here(sw[e], torch.float16, scales, cur), group)
     return packed
 
 

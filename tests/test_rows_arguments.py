@@ -52,3 +52,5 @@ def test_packing_checks_both_operands(group):
             fq.pack_experts(wq, sw, group)
     with pytest.raises(fq.FlexQError):
         fq.pack_experts(codes, fine, 64)
+    apart = torch.ones((E, 2 * N, K), dtype=I8, device="cuda")[:, :N]        # experts that do not follow each other
+    assert torch.equal(fq.pack_experts(apart, fine, group), fq.pack_experts(codes, fine, group))
