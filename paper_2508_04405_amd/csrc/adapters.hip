@@ -18,8 +18,11 @@
 // beside 233 MB), so memory, in rows too short for a tile to be used twice: there the first launch
 // reads x at 2.3 TB/s, 14 us, the second reads y and writes out at 4.2, 48 us.  Few rows: the two
 // launches and their trips to memory, one after the other (one row 3.7 + 4.2 us, 333 rows of
-// 5248 x 13664 at rank 32 5.7 + 9.4).  64 ranks and more with many rows: the loads of A and B from L2,
-// which every 16 or 32 rows repeat (4096 x 4096 of rank 64 43 us at 105 MB).
+// 5248 x 13664 at rank 32 5.6 + 9.3).  In the second these are offsets (two, where rows without an adapter
+// are copied), order, shares of h (a trip for every four splits, added up and split anew by every
+// workgroup of a piece), LDS; then each step over columns waits for the loads and the stores of the
+// one before.  64 ranks and more with many rows: the loads of A and B from L2, which every 16 or 32 rows
+// repeat (4096 x 4096 of rank 64 43 us at 105 MB).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"

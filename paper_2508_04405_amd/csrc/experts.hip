@@ -17,12 +17,17 @@ namespace {
 using flexq::ExpertLinear;
 
 // Few rows an expert: the experts' weights are read once and the products are small change, so a workgroup takes one
-// expert and 32 output channels, whose tiles follow each other in memory, its W wavefronts interleave over them with P
-// tiles each on the way, unpack in registers and multiply by the rows (the MFMA's other 32, rows that are not there
-// cost nothing), and their sums meet in LDS.  More than 32 rows read the weights again, from L2.
-// Bound by HBM and, below some 30 MB, by launch, ramp-up and drain: six experts of 2816 x 2048 for one token,
-// 26 MB, 8.2 us (3.2 TB/s).  Activations go straight to registers: staged in LDS they cost a
-// barrier before the first product and gained nothing.
+// expert and 32 output channels, whose tiles follow each other in memory, its W wavefronts interleave over them, unpack
+// in registers and multiply by the rows (the MFMA's other 32, rows that are not there cost nothing), and their sums
+// meet in LDS.  More than 32 rows walk the weights again, 32 rows a walk, in the same workgroup and by loads that the caches
+// need not keep: an expert far above the others' average holds its workgroups while theirs are done.
+// P tiles are asked for ahead, but in branches, so that the compiler waits for all that is on the way at the head of each
+// step: there is one tile's time in flight, not P.  Ahead of the first weights lie three trips to memory one after
+// the other: offsets, order, token scale.
+// Bound by HBM and, below some 30 MB, by launch, ramp-up (those trips) and drain: six experts of 2816 x 2048 for one
+// token, 26 MB, 8.2 us (3.2 TB/s), 9.6 with group-128 scales; eight of 4096 x 11008 with those at eight tokens, 250 MB,
+// 52 us (4.8).  Activations go straight to registers: staged in LDS they cost a barrier before the first product and
+// gained nothing.
 template <int GROUP, int P, int W>
 __global__ __launch_bounds__(64 * W) void expert_stream_kernel(ExpertLinear a)
 {
@@ -185,9 +190,11 @@ hipError_t launch_stream(const ExpertLinear &a, hipStream_t st)
 // How the rows fall is known on the device only, so by their average over the experts: the kernel that is
 // estimated to be fastest.  An estimate is the busiest CU's stages of 128 k at what a stage takes with so many
 // workgroups on a CU, something a round and a launch, and no less than the touched experts' weights take from
-// memory.  The constants are fitted to 860 random layers (768 .. 12160 deep, 512 .. 22000 wide, 2 .. 128 experts,
-// 1 .. 6000 tokens, 1 .. 8 experts each), which they meet to 10 .. 16 %; on 600 others what is chosen takes 1.025 times the fastest
-// kernel's time on average, 1.12 or less on nine in ten, 1.48 at most.  Some layers, us by form 1 / 2 / 3 / 4 / 5 / 6:
+// memory.  The constants are fitted to 860 random layers (768 .. 12160 deep, 512 .. 22000 wide, 2 .. 128 experts, 16 ..
+// 6000 tokens, 1 .. 8 experts each), which they meet to 10 .. 16 %; on 600 others of 1 .. 300 tokens what is chosen takes
+// 1.028 times the fastest kernel's time on average, 1.12 or less on nine in ten, 1.48 at most.  All of them were routed
+// nearly evenly (experts' scores apart by 0.3 of what they vary by): experts far above the average were not timed, and
+// the streaming kernel suffers most there.  Some layers, us by form 1 / 2 / 3 / 4 / 5 / 6:
 //   2 experts at 16 rows, K 8576, N 1088     12 / 23 / 27 / 37 / 56 / 49
 //   64 at 24 rows, K 2048, N 2816            91 / 50 / 49 / 58 / 56 / -
 //   8 at 128 rows, K 11008, N 4096           - / 119 / 97 / 103 / 96 / 103

@@ -18,16 +18,19 @@
 // 256 experts, spent as many instructions a round on one token: 32768 tokens of 256 by logit 35 us
 // a call, now 25.)
 //
-// What bounds it: instructions, not the 8 MB of logits (2 us).  8192 tokens of 256 experts, sigmoids
-// with a bias, 4 of 8 groups, 8 chosen, are five rounds over groups and nine over experts: 22 us; 333
-// of 60 by softmax 4.4; one token of 8 3.4 with its grouping, a launch and two trips to memory.
+// What bounds it: not the 8 MB of logits (2 us), but the rounds, each a chain that waits for the one
+// before and looks at all of a lane's keys.  Sigmoids of 256 experts with a bias, 4 of 8 groups, 8 chosen,
+// are four rounds over groups and nine over experts: 14 us for 256 tokens, one pass of every wavefront; 22
+// for 8192, where instructions count too, at two wavefronts a SIMD (the second look, inlined, takes the
+// registers to 256); 49 for 32768.  333 of 60 by softmax 4.2; one token of 8 3.3 with its grouping, a launch
+// and two trips to memory.  More than 256 experts spill registers.
 //
 // Grouping is a counting sort, stable, so that equal inputs give equal orders: every block counts
 // its slots per bucket (bucket `count` holds the rows without one), and a second launch adds up the
 // counts of the blocks before it and hands out places -- rank within a wavefront by ballots over the
 // bits of the bucket, wavefronts and blocks by their counts.  No atomics but LDS counters, whose sum
 // has no order.  Few slots: everything in the one block of one launch.  The second launch takes 9.3 us
-// for 65536 slots over 256 experts and 5.0 for 1665 over 60: a chain of barriers and trips to L2 (all
+// for 65536 slots over 256 experts and 4.9 for 1665 over 60: a chain of barriers and trips to L2 (all
 // blocks' counts, 132 KB, are read by every block; bytes to memory 0.8 MB).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
