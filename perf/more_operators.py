@@ -182,6 +182,8 @@ def prepare(case, seed):
             s["blocks"] = fq.Sequences(_starts(s["touched"]), s["lengths_dev"], s["table"], s["slots"])
         if sum(whole):
             fq.cache_append(s["cache"], k, v, fq.Sequences(_starts(whole), torch.tensor(whole, dtype=torch.int32).cuda(), s["table"], s["slots"]))
+        if c["kind"] == "store" and c["new"] > BLOCK:    # (fewer leave the tokens before them where they are)
+            s["before"] = s["cache"].recent.clone()
     else:
         s["codes"] = torch.zeros((2, pages * (page // BLOCK), kv, BLOCK, D), dtype=torch.int8, device="cuda")
         s["scales"] = torch.zeros((2, pages * (page // BLOCK), kv), dtype=torch.float16, device="cuda")
@@ -252,6 +254,8 @@ def run(s):
         if c["kind"] == "prompt":
             return fq.prompt_attention(s["q"], s["k"], s["v"], c["heads"], c["kv"], s["starts"], out=s["out"])
         if c["kind"] == "store":
+            if "before" in s:
+                s["cache"].recent.copy_(s["before"])
             fq.cache_append(s["cache"], s["k"], s["v"], s["seqs"])
             return fq.cache_read(s["cache"], s["blocks"], out=s["back"])
         return fq.cache_attention(s["cache"], s["q"], c["heads"], s["seqs"], out=s["out"])
