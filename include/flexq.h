@@ -15,8 +15,9 @@
  * (Section 4.1.3, "FlexQ System Runtime").
  *
  * Beside it, for batches whose rows choose their own weights: routing of tokens
- * to experts, the experts' linear layers, low-rank adapters of many requests
- * (at the end of this file).
+ * to experts, the experts' linear layers, low-rank adapters of many requests;
+ * and a block's attention: rotation, prompts, an 8-bit cache (at the end of this
+ * file).
  *
  * Conventions for every entry point:
  *   - every pointer marked "dev" is DEVICE memory owned by the caller; the
@@ -469,6 +470,85 @@ size_t flexq_adapters_workspace_bytes(int M, int L, int R, int K);
 flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *scale, int L, int R, const uint16_t *x,
                             const int32_t *order, const int32_t *offsets, int M, int N, int K, const uint16_t *y,
                             uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Between a decoder block's fused QKV linear and its attention output linear (stages 0 and 1 of flexq_layer_linears):
+ * rotation of the heads, attention over prompts, and attention over an 8-bit cache of keys and values.
+ *
+ * head_dim is 64 or 128; `heads` query heads share kv_heads key heads, heads / kv_heads each, in order.  Rows are fp16, one
+ * a token, their heads one after the other; a row stride counts elements, is a multiple of 8 and at least the row's width,
+ * so that the parts of a fused QKV row are taken where they lie.  Pointers to rows are 16-byte aligned, and what is written
+ * overlaps no input unless it says so.  Inputs are finite (rows that belong to no sequence may hold anything).
+ *
+ * flexq_rotate_heads: heads of queries, then of keys, in the first (heads + kv_heads) * head_dim columns of x:
+ *   h = x / sqrt(mean(x^2) + eps) * gamma over each head (gamma_q, gamma_k dev, fp16 [head_dim], 16-byte aligned; NULL: h = x),
+ *   then by position the pairs (h_i, h_(i + rot/2)), with interleaved = 1 (h_2i, h_(2i+1)), i < rot / 2, through the angle
+ *   t = positions[m] * freq[i]:  (a cos t - b sin t, b cos t + a sin t);  elements from rot on are h.
+ *   positions  dev, int32 [M]        freq  dev, fp32 [rot/2], radians a position        rot  a multiple of 16
+ *   out        dev, rows like x, other columns are left as they were; may be x (with the same stride)
+ * fp32 throughout and one rounding; t is taken modulo a turn in 64 bits, so that far positions are as good as near ones.
+ *
+ * SEQUENCES of a batch lie one behind the other in its rows: `starts` (dev, int32 [count + 1], ascending from 0) says where each
+ * begins; rows behind the last are left as they were.  A sequence may have no row.
+ *
+ * flexq_prompt_attention: out_i = sum_j p_ij v_j / sum_j p_ij, p_ij = exp(scale q_i . k_j), over the tokens j up to i
+ * of the same sequence; q, out [M, heads * head_dim], k, v [M, kv_heads * head_dim].  Scores and sums are fp32, p is
+ * rounded to fp16 before it multiplies v.  0 < scale <= 65504 (usually 1 / sqrt(head_dim)).
+ *
+ * THE CACHE holds keys and values of many sequences in pages of `page` tokens (16 to FLEXQ_CACHE_MAX_PAGE, a power of two).
+ * FLEXQ_CACHE_BLOCK tokens of a sequence, from a multiple of it on, are a block; a full block lies in its page as int8 codes
+ * with an fp16 scale for its keys and one for its values of each head (those of flexq_quant_act with 8 bits, for the
+ * 16 * head_dim values together).  The tokens of the unfinished block stay fp16, with the block before it, in a ring that
+ * each sequence has for itself (its slot); so every value is rounded once, whichever way its tokens came, and a sequence
+ * may be shortened again (drafts that were turned down) as far back as to the beginning of the block before the unfinished one.
+ *   codes    dev, 16-byte aligned, pages * flexq_cache_page_bytes(...) bytes: pages are copied and moved as they are
+ *   recent   dev, 16-byte aligned, slots * flexq_cache_recent_bytes(...) bytes: slots likewise
+ * Neither needs to be initialised.  flexq_sequences, beside starts (the batch's rows are the sequences' newest tokens):
+ *   lengths  dev, int32 [count]: tokens of each sequence, the batch's among them
+ *   table    dev, int32 [count][max_pages]: its pages in order.  What a page outside 0 .. pages - 1 would hold is not there:
+ *            appends drop it, attention does not see it, reads give zero.  Entries behind the length are not looked at
+ *   slots    dev, int32 [count], its slot, different ones; outside 0 .. slots - 1 likewise.  NULL: sequence i has slot i
+ * flexq_cache_append   rows k, v [M, kv_heads * head_dim] into the cache.  Pages that sequences share must not be written
+ * flexq_cache_read     the same rows back, as the cache stands for them, in fp16 (65504 at most); starts may name more rows
+ *                      than were appended last, up to whole sequences
+ * flexq_cache_attention  rows of queries over the cache: row i of the n of a sequence of length L sees its tokens
+ *            0 .. L - n + i, out as for prompts, p times a value's scale rounded to fp16.  A row that sees nothing gives zero.
+ *            Any n: generation, drafts, the next chunk of a prompt.  Append first.
+ *   workspace  flexq_cache_attention_workspace_bytes(M, count, heads, kv_heads, head_dim) bytes, 16-byte aligned, any
+ *              content; calls that share it must be ordered on one stream
+ * Results are the same every time.  Lengths, pages and slots are read on the device, by captured graphs too.
+ */
+#define FLEXQ_CACHE_BLOCK 16
+#define FLEXQ_CACHE_MAX_PAGE 1024
+
+typedef struct {
+    int kv_heads, head_dim, page, pages, slots;
+    void *codes;
+    uint16_t *recent;
+} flexq_cache;
+
+typedef struct {
+    int count, max_pages;
+    const int32_t *starts, *lengths, *table, *slots;
+} flexq_sequences;
+
+flexq_status flexq_rotate_heads(const uint16_t *x, int x_stride, int M, int heads, int kv_heads, int head_dim,
+                                const int32_t *positions, const float *freq, int rot, int interleaved,
+                                const uint16_t *gamma_q, const uint16_t *gamma_k, float eps, uint16_t *out, int out_stride,
+                                void *stream);
+flexq_status flexq_prompt_attention(const uint16_t *q, int q_stride, const uint16_t *k, int k_stride, const uint16_t *v,
+                                    int v_stride, const int32_t *starts, int sequences, int M, int heads, int kv_heads,
+                                    int head_dim, float scale, uint16_t *out, int out_stride, void *stream);
+size_t flexq_cache_page_bytes(int kv_heads, int head_dim, int page);
+size_t flexq_cache_recent_bytes(int kv_heads, int head_dim);
+flexq_status flexq_cache_append(const flexq_cache *cache, const flexq_sequences *seqs, int M, const uint16_t *k, int k_stride,
+                                const uint16_t *v, int v_stride, void *stream);
+flexq_status flexq_cache_read(const flexq_cache *cache, const flexq_sequences *seqs, int M, uint16_t *k, int k_stride,
+                              uint16_t *v, int v_stride, void *stream);
+size_t flexq_cache_attention_workspace_bytes(int M, int sequences, int heads, int kv_heads, int head_dim);
+flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequences *seqs, int M, int heads, const uint16_t *q,
+                                   int q_stride, float scale, uint16_t *out, int out_stride, void *workspace,
+                                   size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

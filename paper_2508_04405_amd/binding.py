@@ -39,6 +39,16 @@ class _LayerIO(ctypes.Structure):
                                                "h_attn_norm", "h_ffn_norm", "h_swiglu")]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("kv_heads", "head_dim", "page", "pages", "slots")] + [
+        ("codes", ctypes.c_void_p), ("recent", ctypes.c_void_p)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int), ("max_pages", ctypes.c_int)] + [
+        (n, ctypes.c_void_p) for n in ("starts", "lengths", "table", "slots")]
+
+
 def load():
     """Load libflexq.so, building it first if it is missing or older than its sources."""
     global _lib
@@ -111,6 +121,24 @@ def load():
     lib.flexq_adapters_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
     lib.flexq_adapters.restype = c_int
     lib.flexq_adapters.argtypes = [vp, vp, vp, c_int, c_int, vp, vp, vp, c_int, c_int, c_int, vp, vp, vp, c_size, vp]
+    lib.flexq_rotate_heads.restype = c_int
+    lib.flexq_rotate_heads.argtypes = [vp, c_int, c_int, c_int, c_int, c_int, vp, vp, c_int, c_int, vp, vp, ctypes.c_float, vp,
+                                       c_int, vp]
+    lib.flexq_prompt_attention.restype = c_int
+    lib.flexq_prompt_attention.argtypes = [vp, c_int, vp, c_int, vp, c_int, vp, c_int, c_int, c_int, c_int, c_int, ctypes.c_float,
+                                           vp, c_int, vp]
+    lib.flexq_cache_page_bytes.restype = c_size
+    lib.flexq_cache_page_bytes.argtypes = [c_int, c_int, c_int]
+    lib.flexq_cache_recent_bytes.restype = c_size
+    lib.flexq_cache_recent_bytes.argtypes = [c_int, c_int]
+    for fn in (lib.flexq_cache_append, lib.flexq_cache_read):
+        fn.restype = c_int
+        fn.argtypes = [ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences), c_int, vp, c_int, vp, c_int, vp]
+    lib.flexq_cache_attention_workspace_bytes.restype = c_size
+    lib.flexq_cache_attention_workspace_bytes.argtypes = [c_int] * 5
+    lib.flexq_cache_attention.restype = c_int
+    lib.flexq_cache_attention.argtypes = [ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences), c_int, c_int, vp, c_int,
+                                          ctypes.c_float, vp, c_int, vp, c_size, vp]
     _lib = lib
     return lib
 
@@ -593,3 +621,138 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
     _check(lib.flexq_adapters(a.data_ptr(), b.data_ptr(), scale.data_ptr(), L, R, x.data_ptr(), order.data_ptr(),
                               offsets.data_ptr(), M, N, K, y.data_ptr(), res.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return res
+
+
+# ---- a block's attention: rotation of the heads, prompts, an 8-bit cache ------------------------
+
+def _rows(t, rows, width, dev, exact=True):
+    """A view of fp16 rows, [rows, width] or wider ones with exact = False, each contiguous, on device `dev` -> their stride."""
+    s = t.shape
+    if (t.get_device() != dev or t.dtype != torch.float16 or len(s) != 2 or s[0] != rows or s[1] < width or (exact and s[1] != width)
+            or t.stride(1) != 1):
+        raise FlexQError(f"flexq: expected fp16 rows [{rows}, {width}] on the current device, got {t.dtype} {list(s)} of strides "
+                         f"{list(t.stride())} on {t.device}")
+    return t.stride(0) if rows > 1 else max(t.stride(0), (s[1] + 7) // 8 * 8)
+
+
+def _head_dim(t, heads):
+    width = _sizes(t, ("rows", "width"))[1]
+    if heads < 1 or width % heads != 0:
+        raise FlexQError(f"flexq: rows of {width} are not {heads} heads")
+    return width // heads
+
+
+def rotate_heads(x, heads, kv_heads, head_dim, positions, freq, gamma_q=None, gamma_k=None, eps=1e-5, interleaved=False, out=None):
+    """Queries and keys of fused rows fp16 x [M, >= (heads + kv_heads) * head_dim]: the RMS norm of each head (gamma_q,
+    gamma_k fp16 [head_dim], if given), then the rotation by positions int32 [M] through freq fp32 [rot/2] -> rows like
+    x's first (heads + kv_heads) * head_dim columns; `out` may be x."""
+    lib = load()
+    cur = _current(x)
+    M, width = _sizes(x, ("M", "columns"))[0], (heads + kv_heads) * head_dim
+    stride = _rows(x, M, width, cur, exact=False)
+    _here(positions, torch.int32, (M,), cur)
+    _here(freq, torch.float32, (freq.numel(),), cur)
+    for g in (gamma_q, gamma_k):
+        if g is not None:
+            _here(g, torch.float16, (head_dim,), cur)
+    if out is None:
+        out = torch.empty((M, width), dtype=torch.float16, device=x.device)
+    _check(lib.flexq_rotate_heads(x.data_ptr(), stride, M, heads, kv_heads, head_dim, positions.data_ptr(), freq.data_ptr(),
+                                  2 * freq.numel(), 1 if interleaved else 0, _ptr(gamma_q), _ptr(gamma_k), eps, out.data_ptr(),
+                                  _rows(out, M, width, cur, exact=False), _stream()))
+    return out
+
+
+def prompt_attention(q, k, v, heads, kv_heads, starts, scale=None, out=None):
+    """Causal attention over the sequences of a batch: fp16 rows q [M, heads * D], k and v [M, kv_heads * D], sequence i
+    rows starts[i] .. starts[i + 1] - 1 (int32) -> fp16 [M, heads * D].  scale: 1 / sqrt(D) unless given."""
+    lib = load()
+    cur = _current(q)
+    M, D = q.shape[0], _head_dim(q, heads)
+    count = _sizes(starts, ("sequences + 1",))[0] - 1
+    _here(starts, torch.int32, (count + 1,), cur)
+    qs, ks, vs = _rows(q, M, heads * D, cur), _rows(k, M, kv_heads * D, cur), _rows(v, M, kv_heads * D, cur)
+    if out is None:
+        out = torch.empty((M, heads * D), dtype=torch.float16, device=q.device)
+    _check(lib.flexq_prompt_attention(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, starts.data_ptr(), count, M, heads,
+                                      kv_heads, D, D ** -0.5 if scale is None else scale, out.data_ptr(),
+                                      _rows(out, M, heads * D, cur), _stream()))
+    return out
+
+
+class Cache:
+    """Pages of 8-bit keys and values and the sequences' recent tokens (a flexq_cache; keeps the tensors alive): `codes` uint8
+    [pages, page_bytes] and `recent` uint8 [slots, recent_bytes], whose rows are copied and moved as they are."""
+
+    def __init__(self, pages, page, kv_heads, head_dim, slots, device="cuda"):
+        lib = load()
+        page_bytes, recent_bytes = lib.flexq_cache_page_bytes(kv_heads, head_dim, page), lib.flexq_cache_recent_bytes(kv_heads, head_dim)
+        if page_bytes == 0 or pages < 1 or slots < 1:
+            raise FlexQError("flexq: invalid shape of a cache")
+        self.kv_heads, self.head_dim, self.page, self.pages, self.slots = kv_heads, head_dim, page, pages, slots
+        self.codes = torch.empty((pages, page_bytes), dtype=torch.uint8, device=device)
+        self.recent = torch.empty((slots, recent_bytes), dtype=torch.uint8, device=device)
+        self.c = _Cache(kv_heads, head_dim, page, pages, slots, self.codes.data_ptr(), self.recent.data_ptr())
+
+
+class Sequences:
+    """The sequences whose newest tokens a batch's rows are (a flexq_sequences; keeps the tensors alive): int32 starts
+    [n + 1], lengths [n], table [n, max_pages] and slots [n] (None: sequence i has slot i).  The tensors may be updated in
+    place from step to step."""
+
+    def __init__(self, starts, lengths, table, slots=None):
+        cur, (n, pages) = _current(starts), _sizes(table, ("sequences", "pages"))
+        _here(starts, torch.int32, (n + 1,), cur)
+        _here(lengths, torch.int32, (n,), cur)
+        _here(table, torch.int32, (n, pages), cur)
+        if slots is not None:
+            _here(slots, torch.int32, (n,), cur)
+        self.starts, self.lengths, self.table, self.slots, self.count = starts, lengths, table, slots, n
+        self.c = _Sequences(n, pages, starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), _ptr(slots))
+
+
+def _together(cache, seqs, rows):
+    """The current device, which the cache, the sequences and the rows must be on."""
+    cur = _current(rows)
+    if cache.codes.get_device() != cur or seqs.starts.get_device() != cur:
+        raise FlexQError("flexq: the cache, the sequences and the rows are on different devices")
+    return cur
+
+
+def cache_append(cache, k, v, seqs):
+    """fp16 rows k and v [M, kv_heads * D], the newest tokens of the sequences, into the cache."""
+    cur, width = _together(cache, seqs, k), cache.kv_heads * cache.head_dim
+    M = k.shape[0]
+    _check(load().flexq_cache_append(ctypes.byref(cache.c), ctypes.byref(seqs.c), M, k.data_ptr(), _rows(k, M, width, cur),
+                                     v.data_ptr(), _rows(v, M, width, cur), _stream()))
+
+
+def cache_read(cache, seqs, rows=None, out=None):
+    """The newest tokens of the sequences, as many as `seqs` has rows for each, as the cache stands for them -> fp16 rows
+    (k, v) [rows, kv_heads * D]; `out` = (k, v) to reuse, else `rows` says how many."""
+    width = cache.kv_heads * cache.head_dim
+    if out is None:
+        if rows is None or rows < 1:
+            raise FlexQError("flexq: reading takes `out` or a number of rows")
+        out = tuple(torch.empty((rows, width), dtype=torch.float16, device=cache.codes.device) for _ in range(2))
+    k, v = out
+    cur, M = _together(cache, seqs, k), k.shape[0]
+    _check(load().flexq_cache_read(ctypes.byref(cache.c), ctypes.byref(seqs.c), M, k.data_ptr(), _rows(k, M, width, cur),
+                                   v.data_ptr(), _rows(v, M, width, cur), _stream()))
+    return k, v
+
+
+def cache_attention(cache, q, heads, seqs, scale=None, workspace=None, out=None):
+    """Attention of the sequences' newest tokens, fp16 rows q [M, heads * D], over the cache that holds them already -> fp16
+    [M, heads * D]: row i of n of a sequence of length L sees tokens 0 .. L - n + i.  scale: 1 / sqrt(D) unless given."""
+    lib = load()
+    cur, D = _together(cache, seqs, q), cache.head_dim
+    M = q.shape[0]
+    stride = _rows(q, M, heads * D, cur)
+    ws = _scratch(lib.flexq_cache_attention_workspace_bytes(M, seqs.count, heads, cache.kv_heads, D), workspace, q.device, cur)
+    if out is None:
+        out = torch.empty((M, heads * D), dtype=torch.float16, device=q.device)
+    _check(lib.flexq_cache_attention(ctypes.byref(cache.c), ctypes.byref(seqs.c), M, heads, q.data_ptr(), stride,
+                                     D ** -0.5 if scale is None else scale, out.data_ptr(), _rows(out, M, heads * D, cur),
+                                     ws.data_ptr(), ws.numel(), _stream()))
+    return out

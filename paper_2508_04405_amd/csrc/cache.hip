@@ -1,0 +1,310 @@
+// The cache of keys and values: new tokens' rows into it, and rows read back.
+//
+// Sixteen tokens of a sequence, from a multiple of sixteen on, are a block. A block that is full lies in its page as 8-bit
+// codes, with one scale for its keys and one for its values of a head: the activation quantizer's codes and scales of the
+// 16 D values.  Until then its tokens wait in fp16, in a ring of 32 tokens that every sequence has: so each value is
+// rounded once, whatever way its block filled up, and the ring still holds the block before the unfinished one, to which a
+// sequence may be shortened.
+//
+// A workgroup takes one block of a sequence and head; the one that has a sequence's first block -- the only one that reads
+// tokens from the ring -- also writes the new tokens of its last two into the ring, after it has read.
+//
+// Bound by memory where there are many tokens: 4 bytes of rows in and 2 of codes out for each pair of elements; by the launch
+// and three dependent trips (starts, lengths and page, rows) where there are few.
+#include "../../include/flexq.h"
+#include "flexq_device.h"
+#include "flexq_kernels.h"
+#include "producer_math.h"
+#include "sequences.h"
+
+namespace {
+
+struct AppendArgs {
+    CacheArgs c;
+    const uint16_t *k, *v;
+    size_t k_stride, v_stride;
+};
+
+struct ReadArgs {
+    CacheArgs c;
+    uint16_t *k, *v;
+    size_t k_stride, v_stride;
+};
+
+// Four fp16 values of a channel -> four codes with their bias, one to a byte.
+__device__ __forceinline__ unsigned code4(const uint16_t (&h)[4], float s, float r)
+{
+    unsigned out = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float q = __builtin_amdgcn_fmed3f(__builtin_rintf(div_by(h2f(h[i]), s, r)), -128.0f, 127.0f);
+        out = __builtin_amdgcn_cvt_pk_u8_f32(q + (float)kCodeBias, i, out);
+    }
+    return out;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+{
+    typedef CacheBlock<D> B;
+    constexpr int KEYS = kBlock * D / 8;                 // threads with eight elements of a key
+    __shared__ unsigned top[2][4];
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, head = blockIdx.x % c.kv_heads;
+    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, blockIdx.x / c.kv_heads);
+    if (r.id < 0 || r.n == 0) return;
+    const int length = cached_length(c, r.id), first = length - r.n;         // (may be negative: those rows are dropped)
+    const int b0 = max(first, 0) / kBlock, b = b0 + r.piece, full = length / kBlock;
+    const bool leads = r.piece == 0;
+    if (b >= full && !leads) return;
+    uint16_t *recent = B::recent(c, r.id, head);
+    const uint16_t *k = a.k + (size_t)head * D, *v = a.v + (size_t)head * D;
+    auto row = [&](int token) { return (size_t)(r.begin + (token - first)); };
+    if (b < full) {
+        const int page = B::page_of(c, r.id, b);
+        const int token = tid / (D / 8), d = tid % (D / 8) * 8;              // a key's elements of this thread
+        const int quad = tid / (D / 2), dv = tid % (D / 2) * 2;              // four tokens' values of two channels
+        uint4 kv = make_uint4(0u, 0u, 0u, 0u);
+        unsigned vv[4] = {0u, 0u, 0u, 0u};
+        if (page >= 0) {
+            if (KEYS == 256 || tid < KEYS) {
+                const int t = b * kBlock + token;
+                if (t >= first)
+                    kv = *reinterpret_cast<const uint4 *>(k + row(t) * a.k_stride + d);
+                else if (recent)
+                    kv = *reinterpret_cast<const uint4 *>(recent + B::recent_key(t, d));
+            }
+            if (D == 128 || quad < 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = b * kBlock + 4 * quad + i;
+                    if (t >= first)
+                        vv[i] = *reinterpret_cast<const unsigned *>(v + row(t) * a.v_stride + dv);
+                    else if (recent)
+                        vv[i] = recent[B::recent_value(t, dv)] | ((unsigned)recent[B::recent_value(t, dv + 1)] << 16);
+                }
+            }
+        }
+        unsigned mk = max_bits(kv, 0u), mv = max_bits(make_uint4(vv[0], vv[1], vv[2], vv[3]), 0u);
+        mk = wave_max_bits(mk);
+        mv = wave_max_bits(mv);
+        if ((tid & 63) == 0) {
+            top[0][tid >> 6] = mk;
+            top[1][tid >> 6] = mv;
+        }
+        __syncthreads();
+        if (page >= 0) {
+            mk = max(max(top[0][0], top[0][1]), max(top[0][2], top[0][3]));
+            mv = max(max(top[1][0], top[1][1]), max(top[1][2], top[1][3]));
+            const uint16_t sk = token_scale(h2f((uint16_t)mk), 127.0f), sv = token_scale(h2f((uint16_t)mv), 127.0f);
+            uint8_t *codes = B::codes(c, page, head, b);
+            if (KEYS == 256 || tid < KEYS) {
+                uint2 q = quant8(kv, h2f(sk), 1.0f / h2f(sk), -128.0f, 127.0f);
+                *reinterpret_cast<uint2 *>(codes + key_at(token, d)) = make_uint2(q.x ^ 0x80808080u, q.y ^ 0x80808080u);
+            }
+            if (D == 128 || quad < 4) {
+                const float s = h2f(sv), inv = 1.0f / s;
+                uint16_t lo[4], hi[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    lo[i] = (uint16_t)(vv[i] & 0xffffu);
+                    hi[i] = (uint16_t)(vv[i] >> 16);
+                }
+                uint8_t *values = codes + kBlock * D;
+                *reinterpret_cast<unsigned *>(values + value_at(4 * quad, dv)) = code4(lo, s, inv);
+                *reinterpret_cast<unsigned *>(values + value_at(4 * quad, dv + 1)) = code4(hi, s, inv);
+            }
+            if (tid == 0) *B::scales(c, page, head, b) = (unsigned)sk | ((unsigned)sv << 16);
+        }
+    }
+    if (!leads || !recent) return;
+    __syncthreads();                                     // the ring has been read
+    const int begin = max(max(first, 0), (full - 1) * kBlock);
+    for (int i = tid; i < (length - begin) * (D / 8); i += 256) {
+        const int t = begin + i / (D / 8), d = i % (D / 8) * 8;
+        *reinterpret_cast<uint4 *>(recent + B::recent_key(t, d)) = *reinterpret_cast<const uint4 *>(k + row(t) * a.k_stride + d);
+        const uint4 w = *reinterpret_cast<const uint4 *>(v + row(t) * a.v_stride + d);
+        const unsigned w4[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            recent[B::recent_value(t, d + 2 * j)] = (uint16_t)(w4[j] & 0xffffu);
+            recent[B::recent_value(t, d + 2 * j + 1)] = (uint16_t)(w4[j] >> 16);
+        }
+    }
+}
+
+// fp16 of a code times its scale, the largest finite one where that is beyond them.
+__device__ __forceinline__ unsigned value2(unsigned lo, unsigned hi, float s)
+{
+    return pack_h2(__builtin_amdgcn_fmed3f((float)((int)lo - kCodeBias) * s, -65504.0f, 65504.0f),
+                   __builtin_amdgcn_fmed3f((float)((int)hi - kCodeBias) * s, -65504.0f, 65504.0f));
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
+{
+    typedef CacheBlock<D> B;
+    constexpr int KEYS = kBlock * D / 8;
+    const CacheArgs &c = a.c;
+    const int tid = threadIdx.x, head = blockIdx.x % c.kv_heads;
+    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, blockIdx.x / c.kv_heads);
+    if (r.id < 0 || r.n == 0) return;
+    const int length = cached_length(c, r.id), first = length - r.n;
+    // (first may be negative: the block of a negative token has none, its rows are zero)
+    const int b = (first >> 4) + r.piece, full = length / kBlock;
+    if (b * kBlock >= length) return;
+    uint16_t *ko = a.k + (size_t)head * D, *vo = a.v + (size_t)head * D;
+    auto row = [&](int token) { return (size_t)(r.begin + (token - first)); };
+    const int token = tid / (D / 8), d = tid % (D / 8) * 8, quad = tid / (D / 2), dv = tid % (D / 2) * 2;
+    const bool keys = KEYS == 256 || tid < KEYS, values = D == 128 || quad < 4;
+    uint4 kv = make_uint4(0u, 0u, 0u, 0u);
+    unsigned vv[4] = {0u, 0u, 0u, 0u};
+    if (b >= 0 && b < full) {
+        const int page = B::page_of(c, r.id, b);
+        if (page >= 0) {
+            const uint8_t *codes = B::codes(c, page, head, b);
+            const unsigned s = *B::scales(c, page, head, b);
+            const float sk = h2f((uint16_t)(s & 0xffffu)), sv = h2f((uint16_t)(s >> 16));
+            if (keys) {
+                const uint2 q = *reinterpret_cast<const uint2 *>(codes + key_at(token, d));
+                kv.x = value2(q.x & 255u, q.x >> 8 & 255u, sk);
+                kv.y = value2(q.x >> 16 & 255u, q.x >> 24, sk);
+                kv.z = value2(q.y & 255u, q.y >> 8 & 255u, sk);
+                kv.w = value2(q.y >> 16 & 255u, q.y >> 24, sk);
+            }
+            if (values) {
+                const unsigned lo = *reinterpret_cast<const unsigned *>(codes + kBlock * D + value_at(4 * quad, dv));
+                const unsigned hi = *reinterpret_cast<const unsigned *>(codes + kBlock * D + value_at(4 * quad, dv + 1));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vv[i] = value2(lo >> 8 * i & 255u, hi >> 8 * i & 255u, sv);
+            }
+        }
+    } else if (b >= 0) {
+        if (const uint16_t *recent = B::recent(c, r.id, head)) {
+            if (keys) kv = *reinterpret_cast<const uint4 *>(recent + B::recent_key(b * kBlock + token, d));
+            if (values) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = b * kBlock + 4 * quad + i;
+                    vv[i] = recent[B::recent_value(t, dv)] | ((unsigned)recent[B::recent_value(t, dv + 1)] << 16);
+                }
+            }
+        }
+    }
+    auto mine = [&](int t) { return t >= first && t < length; };
+    if (keys && mine(b * kBlock + token)) *reinterpret_cast<uint4 *>(ko + row(b * kBlock + token) * a.k_stride + d) = kv;
+    if (values) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = b * kBlock + 4 * quad + i;
+            if (mine(t)) *reinterpret_cast<unsigned *>(vo + row(t) * a.v_stride + dv) = vv[i];
+        }
+    }
+}
+
+}  // namespace
+
+namespace flexq {
+
+flexq_status cache_args(const flexq_cache *C, const flexq_sequences *S, int M, CacheArgs &c)
+{
+    if (!C || !S || M < 1) return FLEXQ_EINVAL;
+    if (!C->codes || !C->recent || C->kv_heads < 1 || C->pages < 1 || C->slots < 1) return FLEXQ_EINVAL;
+    if (!S->starts || !S->lengths || !S->table || S->count < 1 || S->max_pages < 1) return FLEXQ_EINVAL;
+    const size_t page_bytes = flexq_cache_page_bytes(C->kv_heads, C->head_dim, C->page);
+    if (page_bytes == 0 || S->count > (1 << 20) || (long)S->max_pages * C->page > (1L << 30)) return FLEXQ_ESHAPE;
+    if (M > (1 << 28)) return FLEXQ_ESHAPE;
+    if ((reinterpret_cast<uintptr_t>(C->codes) & 15u) || (reinterpret_cast<uintptr_t>(C->recent) & 15u) ||
+        (reinterpret_cast<uintptr_t>(S->starts) & 3u) || (reinterpret_cast<uintptr_t>(S->lengths) & 3u) ||
+        (reinterpret_cast<uintptr_t>(S->table) & 3u) || (reinterpret_cast<uintptr_t>(S->slots) & 3u))
+        return FLEXQ_EALIGN;
+    c.codes = (uint8_t *)C->codes;
+    c.recent = C->recent;
+    c.starts = S->starts;
+    c.lengths = S->lengths;
+    c.table = S->table;
+    c.slots = S->slots;
+    c.page_bytes = page_bytes;
+    c.kv_heads = C->kv_heads;
+    c.pages = C->pages;
+    c.slot_count = C->slots;
+    c.shift = __builtin_ctz((unsigned)C->page / kBlock);
+    c.count = S->count;
+    c.max_pages = S->max_pages;
+    c.M = M;
+    return FLEXQ_OK;
+}
+
+}  // namespace flexq
+
+namespace {
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Checks that append and read share; the grid they need.
+flexq_status rows_check(const flexq_cache *C, const flexq_sequences *S, int M, const uint16_t *k, int k_stride, const uint16_t *v,
+                        int v_stride, CacheArgs &c, long &grid)
+{
+    if (!k || !v) return FLEXQ_EINVAL;
+    if (flexq_status s = flexq::cache_args(C, S, M, c); s != FLEXQ_OK) return s;
+    const int width = C->kv_heads * C->head_dim;
+    if (k_stride < width || v_stride < width || k_stride % 8 != 0 || v_stride % 8 != 0) return FLEXQ_ESHAPE;
+    if (!aligned16(k) || !aligned16(v)) return FLEXQ_EALIGN;
+    grid = ((long)M / kBlock + 2L * S->count) * C->kv_heads;
+    return grid < (1L << 24) ? FLEXQ_OK : FLEXQ_ESHAPE;          // 256 threads each, 2^32 a launch
+}
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+size_t flexq_cache_page_bytes(int kv_heads, int head_dim, int page)
+{
+    if (kv_heads < 1 || (head_dim != 64 && head_dim != 128) || (long)kv_heads * head_dim > FLEXQ_MAX_K) return 0;
+    if (page < kBlock || page > FLEXQ_CACHE_MAX_PAGE || (page & (page - 1)) != 0) return 0;
+    return ((size_t)(page / kBlock) * kv_heads * (2 * kBlock * head_dim + 4) + 255) / 256 * 256;
+}
+
+size_t flexq_cache_recent_bytes(int kv_heads, int head_dim)
+{
+    if (kv_heads < 1 || (head_dim != 64 && head_dim != 128) || (long)kv_heads * head_dim > FLEXQ_MAX_K) return 0;
+    return (size_t)kv_heads * 4 * kBlock * head_dim * 2;
+}
+
+flexq_status flexq_cache_append(const flexq_cache *cache, const flexq_sequences *seqs, int M, const uint16_t *k, int k_stride,
+                                const uint16_t *v, int v_stride, void *stream)
+{
+    AppendArgs a{};
+    long grid = 0;
+    if (flexq_status s = rows_check(cache, seqs, M, k, k_stride, v, v_stride, a.c, grid); s != FLEXQ_OK) return s;
+    a.k = k;
+    a.v = v;
+    a.k_stride = (size_t)k_stride;
+    a.v_stride = (size_t)v_stride;
+    if (cache->head_dim == 128)
+        hipLaunchKernelGGL(append_kernel<128>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+    else
+        hipLaunchKernelGGL(append_kernel<64>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+flexq_status flexq_cache_read(const flexq_cache *cache, const flexq_sequences *seqs, int M, uint16_t *k, int k_stride,
+                              uint16_t *v, int v_stride, void *stream)
+{
+    ReadArgs a{};
+    long grid = 0;
+    if (flexq_status s = rows_check(cache, seqs, M, k, k_stride, v, v_stride, a.c, grid); s != FLEXQ_OK) return s;
+    a.k = k;
+    a.v = v;
+    a.k_stride = (size_t)k_stride;
+    a.v_stride = (size_t)v_stride;
+    if (cache->head_dim == 128)
+        hipLaunchKernelGGL(read_kernel<128>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+    else
+        hipLaunchKernelGGL(read_kernel<64>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

@@ -1,0 +1,272 @@
+// Causal attention over prompts packed one behind the other:
+//
+//   out_i = sum_{j <= i} p_ij v_j / sum_j p_ij,   p_ij = exp(scale q_i . k_j),   j in token i's sequence.
+//
+// Rows of a tile are the tokens of a sequence times the heads that share a key head, 32 a wavefront, so that grouped heads
+// share the keys a workgroup stages and a short prompt fills a tile.  Keys and values come 64 at a time into LDS (direct
+// loads, two buffers, chunks of 16 bytes swizzled by the row); rows past the sequence's end read as zero.  S^T = K Q^T by
+// 32x32x16 MFMAs: a lane holds 32 scores of one row, its other half lane l ^ 32, so that the running maximum is one exchange and
+// everything else stays in the lane.  Its scores in the order of the registers are the column operand of O^T = V^T P^T for
+// keys {0..3, 8..11} + 4 (l / 32) of every sixteen; the row operand is read from LDS transposed, in that order of keys.
+//
+// p enters the MFMA in fp16 times 2^9 and the running maximum is only raised once a score passes it by 6 (powers of two): p
+// is at most 2^15 there and normal down to 2^-23 of that, and the output is rarely rescaled.  The sum of p is fp32,
+// unrounded.
+#include "../../include/flexq.h"
+#include "flexq_device.h"
+#include "flexq_kernels.h"
+#include "gemm_common.h"
+#include "producer_math.h"
+#include "sequences.h"
+
+namespace {
+
+constexpr int kKeys = 64;                        // of a stage
+constexpr float kNothing = -1e30f;
+constexpr float kShift = 9.0f, kLag = 6.0f;
+
+struct PromptArgs {
+    const uint16_t *q, *k, *v;
+    uint16_t *out;
+    const int32_t *starts;
+    size_t q_stride, k_stride, v_stride, out_stride;
+    int M, count, group, kv_heads;
+    float scale;                                 // times log2 e
+};
+
+__device__ __forceinline__ v16f mfma_h(v8h a, v8h b, v16f c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// A lane's four keys of one channel, of 16 lanes' four channels of one key each.
+__device__ __forceinline__ v4h read_transposed(const uint8_t *at)
+{
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s *lds_ptr;
+    union {
+        v4s s;
+        v4h h;
+    } x;
+    x.s = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+    return x.h;
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
+{
+    constexpr int ROWS = 32 * WAVES, LINE = 2 * D, CH = D / 8;           // LINE: bytes of a staged row; CH: its chunks
+    constexpr int STAGE = kKeys * LINE, DMA = STAGE / 1024 / WAVES;      // DMA: loads of a wavefront for keys, or values
+    static_assert(STAGE % (1024 * WAVES) == 0, "a stage is whole loads of every wavefront");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][STAGE];  // [buffer][keys, values]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, i32 = lane & 31;
+    const int head = blockIdx.x % a.kv_heads;
+    const int pieces = gridDim.x / a.kv_heads;
+    // the tiles with most keys first
+    const RowRange r = find_rows(a.starts, a.count, a.M, a.group, ROWS, 1, pieces - 1 - (int)(blockIdx.x / a.kv_heads));
+    if (r.id < 0) return;
+    const int all = r.n * a.group, row0 = r.piece * ROWS;
+    if (row0 >= all) return;
+    const int rows = min(ROWS, all - row0);
+    const int keys = (row0 + rows - 1) / a.group + 1;                    // that the last row sees
+    const int stages = (keys + kKeys - 1) / kKeys;
+    // this lane's row, and what its wavefront sees
+    const int row = row0 + min(32 * wave + i32, rows - 1), token = row / a.group;
+    const bool mine = 32 * wave + i32 < rows;
+    const int w_first = row0 + 32 * wave, w_last = row0 + min(32 * wave + 31, rows - 1);
+    const int sees_all = w_first / a.group, sees_any = 32 * wave < rows ? w_last / a.group : -1;
+    const int q_head = head * a.group + row - token * a.group;
+    v8h q[D / 16];
+    {
+        const uint16_t *from = a.q + (size_t)(r.begin + token) * a.q_stride + (size_t)q_head * D + 8 * half;
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 16 * m);
+    }
+    // stages: load i of a wavefront fills 1 KiB, lane l 16 bytes at 16 l, and so fetches the chunk that the swizzle keeps there
+    int s_row[DMA], k_chunk[DMA], v_chunk[DMA];
+#pragma unroll
+    for (int i = 0; i < DMA; ++i) {
+        const int at = (wave * DMA + i) * 64 + lane, line = at / CH, c = at % CH;
+        s_row[i] = line;
+        k_chunk[i] = c ^ (D == 128 ? line & 15 : (line >> 1) & 7);
+        v_chunk[i] = c ^ (D == 128 ? 2 * (line & 7) : 2 * (line & 3));
+    }
+    const uint16_t *k0 = a.k + (size_t)r.begin * a.k_stride + (size_t)head * D;
+    const uint16_t *v0 = a.v + (size_t)r.begin * a.v_stride + (size_t)head * D;
+    auto fetch = [&](int stage, int buf) {
+        const int left = min(kKeys, r.n - stage * kKeys);                // rows of the sequence there are
+        const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(k0 + (size_t)stage * kKeys * a.k_stride), 0, (unsigned)((left - 1) * (int)a.k_stride * 2 + LINE), 0x00020000);
+        const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(v0 + (size_t)stage * kKeys * a.v_stride), 0, (unsigned)((left - 1) * (int)a.v_stride * 2 + LINE), 0x00020000);
+        const unsigned beyond = 0x7fffffffu;                             // of any stage's rows: reads as zero
+#pragma unroll
+        for (int i = 0; i < DMA; ++i) {
+            uint8_t *dst = &lds[buf][0][(wave * DMA + i) * 1024];
+            const unsigned off = s_row[i] < left ? (unsigned)(s_row[i] * (int)a.k_stride * 2 + 16 * k_chunk[i]) : beyond;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (void __attribute__((address_space(3))) *)dst, 16, off, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < DMA; ++i) {
+            uint8_t *dst = &lds[buf][1][(wave * DMA + i) * 1024];
+            const unsigned off = s_row[i] < left ? (unsigned)(s_row[i] * (int)a.v_stride * 2 + 16 * v_chunk[i]) : beyond;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (void __attribute__((address_space(3))) *)dst, 16, off, 0, 0, 0);
+        }
+    };
+    v16f o[D / 32];
+    float top = kNothing, sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+    fetch(0, 0);
+    for (int stage = 0; stage < stages; ++stage) {
+        const int buf = stage & 1;
+        wait_vmcnt<0>();
+        lds_barrier();                           // everyone's loads of this stage are there, and everyone is done with the last one
+        if (stage + 1 < stages) fetch(stage + 1, buf ^ 1);
+        const int first = stage * kKeys;
+        if (first > sees_any) continue;
+        const uint8_t *ks = lds[buf][0], *vs = lds[buf][1];
+        v16f s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) {
+                const int line = 32 * b + i32;
+                const int c = (2 * m + half) ^ (D == 128 ? line & 15 : (line >> 1) & 7);
+                s[b] = mfma_h(*reinterpret_cast<const v8h *>(ks + line * LINE + 16 * c), q[m], s[b]);
+            }
+        }
+        if (first + kKeys - 1 > sees_all) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (first + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) > token) s[b][i] = -INFINITY;
+        }
+        float best = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) best = fmaxf(best, s[0][i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) best = fmaxf(best, s[1][i]);
+        {
+            auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+            best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.scale;
+        }
+        if (__any(best > top + kLag)) {
+            const float next = fmaxf(top, best), f = __builtin_amdgcn_exp2f(top - next);
+            top = next;
+            sum *= f;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        }
+        const float less = top - kShift;
+        v8h p[2][2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                union {
+                    v2h h[4];
+                    v8h v;
+                } x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * u + 2 * i], a.scale, -less));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * u + 2 * i + 1], a.scale, -less));
+                    sum += e0;
+                    sum += e1;
+                    x.h[i] = __builtin_convertvector((v2f{e0, e1}), v2h);
+                }
+                p[b][u] = x.v;
+            }
+        // lane (dsub, h) of sixteen lanes each: keys 4 h + 0 .. 3 (and 8 more on) of channels 16 dsub .. + 15
+        const int h = lane >> 5, dsub = lane >> 4 & 1, e = lane >> 2 & 3, c4 = lane & 3;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) {
+                    union {
+                        v4h h[2];
+                        v8h v;
+                    } x;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        const int line = 32 * b + 16 * u + 8 * w + 4 * h + e;
+                        const int c = (4 * t + 2 * dsub + (c4 >> 1)) ^ (D == 128 ? 2 * (line & 7) : 2 * (line & 3));
+                        x.h[w] = read_transposed(vs + line * LINE + 16 * c + 8 * (c4 & 1));
+                    }
+                    o[t] = mfma_h(x.v, p[b][u], o[t]);
+                }
+    }
+    {
+        auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+        sum = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    if (!mine) return;
+    const float inv = 1.0f / sum;
+    uint16_t *out = a.out + (size_t)(r.begin + token) * a.out_stride + (size_t)q_head * D + 4 * half;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2 *>(out + 32 * t + 8 * i) = make_uint2(
+                pack_h2(o[t][4 * i] * inv, o[t][4 * i + 1] * inv), pack_h2(o[t][4 * i + 2] * inv, o[t][4 * i + 3] * inv));
+}
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+}  // namespace
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+flexq_status flexq_prompt_attention(const uint16_t *q, int q_stride, const uint16_t *k, int k_stride, const uint16_t *v,
+                                    int v_stride, const int32_t *starts, int sequences, int M, int heads, int kv_heads,
+                                    int head_dim, float scale, uint16_t *out, int out_stride, void *stream)
+{
+    if (!q || !k || !v || !starts || !out || sequences < 1 || M < 1 || heads < 1 || kv_heads < 1) return FLEXQ_EINVAL;
+    if (heads % kv_heads != 0 || !(scale > 0.0f && scale <= 65504.0f)) return FLEXQ_EINVAL;
+    if ((head_dim != 64 && head_dim != 128) || (long)heads * head_dim > FLEXQ_MAX_K) return FLEXQ_ESHAPE;
+    const int width = heads * head_dim, kv_width = kv_heads * head_dim;
+    if (q_stride < width || out_stride < width || k_stride < kv_width || v_stride < kv_width) return FLEXQ_ESHAPE;
+    if (q_stride % 8 != 0 || out_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0) return FLEXQ_ESHAPE;
+    // (a stage's rows are addressed with 32 bits)
+    if (k_stride > (1 << 23) || v_stride > (1 << 23) || sequences > (1 << 20)) return FLEXQ_ESHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(starts)) return FLEXQ_EALIGN;
+    PromptArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = out;
+    a.starts = starts;
+    a.q_stride = (size_t)q_stride;
+    a.k_stride = (size_t)k_stride;
+    a.v_stride = (size_t)v_stride;
+    a.out_stride = (size_t)out_stride;
+    a.M = M;
+    a.count = sequences;
+    a.group = heads / kv_heads;
+    a.kv_heads = kv_heads;
+    a.scale = scale * 1.44269504088896341f;
+    if ((long)M * a.group >= (1L << 30)) return FLEXQ_ESHAPE;
+    constexpr int waves = 4;
+    const long grid = ((long)M * a.group / (32 * waves) + sequences) * kv_heads;
+    if (grid * 64 * waves >= (1L << 32)) return FLEXQ_ESHAPE;            // threads of a launch
+    auto launch = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * waves), 0, (hipStream_t)stream, a);
+    };
+    head_dim == 128 ? launch(prompt_kernel<128, waves>) : launch(prompt_kernel<64, waves>);
+    return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
+}
+
+}  // extern "C"
+#pragma GCC visibility pop
