@@ -25,7 +25,7 @@
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;                        // of a workgroup of the streaming kernel
 constexpr float kNothing = -1e30f;               // running maximum where no key was seen
 constexpr float kShift = 14.0f;                  // p enters the MFMA as p 2^14
 
@@ -34,93 +34,77 @@ struct CachedArgs {
     const uint16_t *q;
     uint16_t *out;
     size_t q_stride, out_stride;
-    float *part;                                 // [kv_heads][parts][2][16 RB rows][D + 4]: output, running maximum, sum
+    float *part;                                 // [kv_heads][parts][2][rows of a tile][D + 4]: output, running maximum, sum
     float scale;                                 // times log2 e
     int group, heads, parts;                     // heads of a key head; workgroups of a key head
     int least;                                   // steps that a workgroup takes at least
 };
 
-// Tiles of a sequence and the steps of each (pairs of blocks; every tile counts as many as the last one has).
-struct Span {
-    int tiles, steps;
-};
-
-template <int ROWS>
-__device__ __forceinline__ Span span_of(const CachedArgs &a, int begin, int end, int length)
-{
-    const int n = max(min(end, a.c.M) - max(begin, 0), 0);
-    Span s;
-    s.tiles = (n * a.group + ROWS - 1) / ROWS;
-    s.steps = (length + 2 * kBlock - 1) / (2 * kBlock);
-    if (s.steps == 0) s.steps = 1;               // (its rows are zero, and written by someone)
-    return s;
-}
-
-// The place of step `at` of a key head's steps: whose tile it falls in, and the tile's first step.
+// Where the steps of a call's tiles lie: those of sequence s follow those of the sequences before it, tile after tile; a
+// tile of ROWS rows has as many of KEYS keys as its sequence's length takes (one, if it has none: someone writes its rows).  A lane
+// holds one of 64 sequences, and where they are more than 64, every question goes through all of them again.
 struct Place {
-    int id, begin, n, length, tile, tiles, steps;
-    long tile_first;                             // step of the row of all at which the tile begins
+    int id, begin, n, length, tile, steps;
+    int first;                                   // step of all at which the tile begins
 };
 
-template <int ROWS>
-__device__ __forceinline__ long all_steps(const CachedArgs &a)
-{
-    long total = 0;
-    for (int s0 = 0; s0 < a.c.count; s0 += 64) {
-        const int s = min(s0 + (int)(threadIdx.x & 63), a.c.count - 1);
-        const Span w = span_of<ROWS>(a, a.c.starts[s], a.c.starts[s + 1], cached_length(a.c, s));
-        long mine = s0 + (int)(threadIdx.x & 63) < a.c.count ? (long)w.tiles * w.steps : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d, 64);
-        total += mine;
-    }
-    return total;
-}
+template <int ROWS, int KEYS>
+struct Steps {
+    const CachedArgs &a;
+    int begin, end, length, tiles, steps, first; // of this lane's sequence; first: of its steps among those of the 64
 
-template <int ROWS>
-__device__ __forceinline__ Place find_step(const CachedArgs &a, long at)
-{
-    const int lane = threadIdx.x & 63;
-    long before = 0;
-    for (int s0 = 0; s0 < a.c.count; s0 += 64) {
-        const int s = min(s0 + lane, a.c.count - 1);
-        const int begin = a.c.starts[s], end = a.c.starts[s + 1], length = cached_length(a.c, s);
-        const Span w = span_of<ROWS>(a, begin, end, length);
-        const long mine = s0 + lane < a.c.count ? (long)w.tiles * w.steps : 0;
-        long sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const long other = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += other;
-        }
-        const long first = before + sum - mine;
-        const unsigned long long hit = __ballot(at >= first && at < first + mine);
-        if (hit) {
-            const int l = __ffsll(hit) - 1;
-            Place p;
-            p.id = s0 + l;
-            p.begin = max(__builtin_amdgcn_readlane(begin, l), 0);
-            p.n = min(__builtin_amdgcn_readlane(end, l), a.c.M) - p.begin;
-            p.length = __builtin_amdgcn_readlane(length, l);
-            p.tiles = __builtin_amdgcn_readlane(w.tiles, l);
-            p.steps = __builtin_amdgcn_readlane(w.steps, l);
-            const long from = __shfl(first, l, 64);
-            p.tile = (int)((at - from) / p.steps);
-            p.tile_first = from + (long)p.tile * p.steps;
-            return p;
-        }
-        before += __shfl(sum, 63, 64);
-    }
-    Place p{};
-    p.id = -1;
-    return p;
-}
+    __device__ __forceinline__ Steps(const CachedArgs &args) : a(args) {}
 
-// Workgroups that share the steps, and where the part of one begins: part i of n is at / n rounded down.
-__device__ __forceinline__ int parts_of_all(const CachedArgs &a, long total)
+    __device__ __forceinline__ int load(int s0)  // -> the steps of all 64
+    {
+        const int lane = threadIdx.x & 63, s = min(s0 + lane, a.c.count - 1);
+        begin = max(a.c.starts[s], 0);
+        end = min(a.c.starts[s + 1], a.c.M);
+        length = cached_length(a.c, s);
+        tiles = s0 + lane < a.c.count ? (max(end - begin, 0) * a.group + ROWS - 1) / ROWS : 0;
+        steps = max((length + KEYS - 1) / KEYS, 1);
+        const int sum = wave_scan(tiles * steps);
+        first = sum - tiles * steps;
+        return __builtin_amdgcn_readlane(sum, 63);
+    }
+    __device__ __forceinline__ int all()
+    {
+        int total = 0;
+        for (int s0 = 0; s0 < a.c.count; s0 += 64) total += load(s0);
+        return total;
+    }
+    __device__ __forceinline__ Place find(int at)        // (after all(); at below it)
+    {
+        Place p{};
+        p.id = -1;
+        int before = 0;
+        for (int s0 = 0; s0 < a.c.count; s0 += 64) {
+            const int lane = threadIdx.x & 63;
+            int sum = 0;
+            if (a.c.count > 64) sum = load(s0);
+            const unsigned long long hit = __ballot(at - before >= first && at - before < first + tiles * steps);
+            if (hit) {
+                const int l = __ffsll(hit) - 1;
+                p.id = s0 + l;
+                p.begin = __builtin_amdgcn_readlane(begin, l);
+                p.n = __builtin_amdgcn_readlane(end, l) - p.begin;
+                p.length = __builtin_amdgcn_readlane(length, l);
+                p.steps = __builtin_amdgcn_readlane(steps, l);
+                const int from = before + __builtin_amdgcn_readlane(first, l);
+                p.tile = (at - from) / p.steps;
+                p.first = from + p.tile * p.steps;
+                return p;
+            }
+            before += sum;
+        }
+        return p;
+    }
+};
+
+// Part i of the steps is i * width .. (i + 1) * width - 1.
+__device__ __forceinline__ int part_width(const CachedArgs &a, int total)
 {
-    const long most = (total + a.least - 1) / a.least;
-    return (int)(most < a.parts ? most : a.parts);
+    return max((total + a.parts - 1) / a.parts, a.least);
 }
 
 __device__ __forceinline__ v4f mfma_h(v8h a, v8h b, v4f c)
@@ -241,8 +225,15 @@ __device__ __forceinline__ void store_row(const CachedArgs &a, int begin, int ro
     *reinterpret_cast<uint2 *>(out) = make_uint2(pack_h2(y[0], y[1]), pack_h2(y[2], y[3]));
 }
 
+// Two blocks of 16 keys and values, as a lane has them.
+template <int D>
+struct Stage {
+    v4u k[2][D / 64], v[2][D / 64];
+    unsigned scales[2];                          // the key's, the value's << 16
+};
+
 template <int D, int RB>
-__global__ __launch_bounds__(64 * kWaves) void cached_kernel(CachedArgs a)
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void cached_kernel(CachedArgs a)
 {
     typedef CacheBlock<D> B;
     constexpr int ROWS = 16 * RB, P = D / 64;    // P: planes of keys, and of values, of a block
@@ -251,16 +242,15 @@ __global__ __launch_bounds__(64 * kWaves) void cached_kernel(CachedArgs a)
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i16 = lane & 15;
     const int head = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
-    const long total = all_steps<ROWS>(a);
-    const int parts = parts_of_all(a, total);
-    if (index >= parts) return;
-    long at = total * index / parts;
-    const long stop = total * (index + 1) / parts;
+    Steps<ROWS, 2 * kBlock> all(a);
+    const int total = all.all(), width = part_width(a, total);
+    int at = index * width;
+    const int stop = min(at + width, total);
     while (at < stop) {
-        const Place p = find_step<ROWS>(a, at);
+        const Place p = all.find(at);
         if (p.id < 0) return;
-        const long end = min(stop, p.tile_first + p.steps);
-        const int first = (int)(at - p.tile_first), last = (int)(end - p.tile_first);    // steps of the tile
+        const int end = min(stop, p.first + p.steps);
+        const int first = at - p.first, last = end - p.first;                // steps of the tile
         const bool whole = first == 0 && last == p.steps;
         const int rows = min(ROWS, p.n * a.group - p.tile * ROWS);
         // rows of this lane: token, position, query
@@ -283,46 +273,88 @@ __global__ __launch_bounds__(64 * kWaves) void cached_kernel(CachedArgs a)
             for (int t = 0; t < D / 16; ++t) r.o[k][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         }
         const int full = p.length / kBlock;                                  // blocks in pages
-        const int seen = (p.length - p.n + (p.tile * ROWS + rows - 1) / a.group) + 1;   // keys that any of the rows sees
+        const int sees_first = p.length - p.n + p.tile * ROWS / a.group;     // last key that the first row sees
+        const int seen = p.length - p.n + (p.tile * ROWS + rows - 1) / a.group + 1;      // keys that any of the rows sees
         const int blocks = min(full, (max(seen, 0) + kBlock - 1) / kBlock);
-        for (int s = first + wave; s < last; s += kWaves) {
-            if (2 * s >= blocks) break;
-            v4u kw[2][P], vw[2][P];
-            float ks[2], lv[2];
-            int from[2];                                                     // first key of a block; beyond all where there is none
+        const int done = min(last, (blocks + 1) / 2);                        // steps over pages end here
+        // pages a step ahead of the loads, loads a step ahead of the products; steps past the end repeat the last block
+        auto pages = [&](int (&page)[2], int s) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) page[b] = c.table[(size_t)p.id * c.max_pages + (min(2 * s + b, blocks - 1) >> c.shift)];
+        };
+        auto load = [&](Stage<D> &st, int (&page)[2], int s) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int block = min(2 * s + b, blocks - 1);
-                const int page = B::page_of(c, p.id, block);
-                const uint8_t *codes = B::codes(c, max(page, 0), head, block);
-                const unsigned sc = *B::scales(c, max(page, 0), head, block);
-                from[b] = page < 0 || 2 * s + b >= blocks ? 0x40000000 : block * kBlock;
+                page[b] = __builtin_amdgcn_readfirstlane(page[b]);
+                if (page[b] < 0 || page[b] >= c.pages) page[b] = -1;
+                const uint8_t *codes = B::codes(c, max(page[b], 0), head, block);
+                st.scales[b] = *B::scales(c, max(page[b], 0), head, block);
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    kw[b][j] = *reinterpret_cast<const v4u *>(codes + 1024 * j + 16 * lane);
-                    vw[b][j] = *reinterpret_cast<const v4u *>(codes + kBlock * D + 1024 * j + 16 * lane);
-                }
-                ks[b] = page < 0 ? 0.0f : h2f((uint16_t)(sc & 0xffffu)) * a.scale;
-                lv[b] = page < 0 ? 0.0f : __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16)));
+                for (int j = 0; j < P; ++j) st.k[b][j] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(codes + 1024 * j) + lane);
+#pragma unroll
+                for (int j = 0; j < P; ++j) st.v[b][j] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(codes + kBlock * D + 1024 * j) + lane);
             }
-            float x[RB][2][4];
+        };
+        auto work = [&](const Stage<D> &st, const int (&page)[2], int s) {
+            float x[RB][2][4], lv[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                const int key = 16 * (2 * s + b);
+                const float ks = h2f((uint16_t)(st.scales[b] & 0xffffu)) * a.scale;
+                lv[b] = __builtin_amdgcn_logf(h2f((uint16_t)(st.scales[b] >> 16)));
                 v4f acc[RB];
 #pragma unroll
                 for (int k = 0; k < RB; ++k) acc[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int m = 0; m < D / 32; ++m) {
-                    const v8h key = codes_to_half(kw[b][m / 2][2 * (m & 1)], kw[b][m / 2][2 * (m & 1) + 1]);
+                    const v8h w = codes_to_half(st.k[b][m / 2][2 * (m & 1)], st.k[b][m / 2][2 * (m & 1) + 1]);
 #pragma unroll
-                    for (int k = 0; k < RB; ++k) acc[k] = mfma_h(key, q[k][m], acc[k]);
+                    for (int k = 0; k < RB; ++k) acc[k] = mfma_h(w, q[k][m], acc[k]);
                 }
+                const bool there = page[b] >= 0 && 2 * s + b < blocks;
+                if (there && key + 15 <= sees_first) {
 #pragma unroll
-                for (int k = 0; k < RB; ++k)
+                    for (int k = 0; k < RB; ++k)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[k][b][i] = from[b] + 4 * g + i <= limit[k] ? acc[k][i] * ks[b] : -INFINITY;
+                        for (int i = 0; i < 4; ++i) x[k][b][i] = acc[k][i] * ks;
+                } else {
+                    if (!there) lv[b] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < RB; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x[k][b][i] = there && key + 4 * g + i <= limit[k] ? acc[k][i] * ks : -INFINITY;
+                }
             }
-            take(r, x, lv[0], lv[1], [&](int t) { return codes_to_half(vw[0][t / 4][t % 4], vw[1][t / 4][t % 4]); });
+            take(r, x, lv[0], lv[1], [&](int t) { return codes_to_half(st.v[0][t / 4][t % 4], st.v[1][t / 4][t % 4]); });
+        };
+        int s = first + wave;
+        if (s < done) {
+            constexpr int N = 2;                         // (three or four: no faster)
+            Stage<D> st[N];
+            int page[N][2], next[2];
+#pragma unroll
+            for (int u = 0; u < N; ++u) pages(page[u], s + u * kWaves);
+#pragma unroll
+            for (int u = 0; u < N - 1; ++u) load(st[u], page[u], s + u * kWaves);
+            for (bool more = true; more;) {
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    pages(next, s + N * kWaves);
+                    load(st[(u + N - 1) % N], page[(u + N - 1) % N], s + (N - 1) * kWaves);
+                    asm volatile("" ::: "memory");                           // (else the loads sink to their use)
+                    __builtin_amdgcn_sched_barrier(0);
+                    work(st[u], page[u], s);
+                    page[u][0] = next[0];
+                    page[u][1] = next[1];
+                    s += kWaves;
+                    if (s >= done) {
+                        more = false;
+                        break;
+                    }
+                }
+            }
         }
         // the unfinished block's tokens, in fp16, with the tile's last step
         const int tail = p.length - full * kBlock;
@@ -403,60 +435,346 @@ __global__ __launch_bounds__(64 * kWaves) void cached_kernel(CachedArgs a)
     }
 }
 
-// Tiles that several workgroups took: their shares in order.  Workgroup (i, r) joins rows r, r + slices, .. of the tile that
-// begins in part i and does not end there, if there is one.
-template <int D, int RB>
-__global__ __launch_bounds__(256) void join_kernel(CachedArgs a, int slices)
+// Many rows: 128 of a tile, 32 a wavefront, and 64 keys a stage that all of them share.  The codes of the next stage are asked for
+// while this one is worked on, and put into LDS as fp16 behind it (two buffers), in the order in which the 32x32x16 MFMAs of the
+// prompts' kernel read them, so that a code is turned once for 128 rows.  A block of 16 keys is half of a result's
+// registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is raised only where a lane's weights of
+// a block add up to more than 2^15.
+constexpr int kStageKeys = 64, kStageBlocks = 4, kStageWaves = 4, kStageRows = 32 * kStageWaves;
+constexpr float kStageShift = 9.0f, kMost = 32768.0f;
+
+__device__ __forceinline__ v16f mfma_h(v8h a, v8h b, v16f c)
 {
-    constexpr int ROWS = 16 * RB, Q = D / 4;     // Q: threads of a row
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_eu(2))) void chunk_kernel(CachedArgs a)
+{
+    typedef CacheBlock<D> B;
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    // keys: a line of D channels each; values: a line of 64 keys for each channel, chunk 2 b + half of 16 bytes holding keys
+    // 16 b + 4 half + {0 .. 3, 8 .. 11}; chunks XORed by the line, so that sixteen lines' same chunk meets every bank once
+    constexpr int LINE = 2 * D, KSTAGE = kStageKeys * LINE, VSTAGE = D * 2 * kStageKeys;
+    constexpr int TASKS = kStageBlocks * D / 64 / kStageWaves;           // planes of 1 KiB of a wavefront, of keys and of values
+    static_assert(TASKS >= 1, "every wavefront has a plane");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][KSTAGE + VSTAGE];
     const CacheArgs &c = a.c;
-    const int head = blockIdx.x % c.kv_heads, slice = blockIdx.x / c.kv_heads % slices, index = blockIdx.x / c.kv_heads / slices;
-    const long total = all_steps<ROWS>(a);
-    const int parts = parts_of_all(a, total);
-    if (index + 1 >= parts) return;
-    const long start = total * index / parts, stop = total * (index + 1) / parts;
-    const Place p = find_step<ROWS>(a, stop);
-    if (p.id < 0 || p.tile_first >= stop || p.tile_first < start) return;
-    const long to = p.tile_first + p.steps;
-    int last = index + 1;                        // the last part that has some of the tile
-    while (last + 1 < parts && total * (last + 1) / parts < to) ++last;
-    const int rows = min(ROWS, p.n * a.group - p.tile * ROWS);
-    const int d = threadIdx.x % Q * 4;
-    for (int row = slice + slices * (int)(threadIdx.x / Q); row < rows; row += slices * (256 / Q)) {
-        float m = kNothing, l = 0.0f;
-        v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = index; i <= last; ++i) {
-            const float *part = a.part + ((((size_t)head * a.parts + i) * 2 + (i == index ? 1 : 0)) * ROWS + row) * (D + 4);
-            const v4f oi = *reinterpret_cast<const v4f *>(part + d);
-            const float mi = part[D], li = part[D + 1];
-            const float top = fmaxf(m, mi), f = __builtin_amdgcn_exp2f(m - top), fi = __builtin_amdgcn_exp2f(mi - top);
-            m = top;
-            l = l * f + li * fi;
-            o = o * f + oi * fi;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
+    const int head = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
+    auto key_swizzle = [](int line) { return D == 128 ? line & 15 : (line >> 1) & 7; };
+    auto value_swizzle = [](int line) { return (line >> 1) & 7; };
+    Steps<kStageRows, kStageKeys> all(a);
+    const int total = all.all(), width = part_width(a, total);
+    int at = index * width;
+    const int stop = min(at + width, total);
+    while (at < stop) {
+        const Place p = all.find(at);
+        if (p.id < 0) return;
+        const int end = min(stop, p.first + p.steps);
+        const int first = at - p.first, last = end - p.first;            // stages of the tile
+        const bool whole = first == 0 && last == p.steps;
+        const int row0 = p.tile * kStageRows, rows = min(kStageRows, p.n * a.group - row0);
+        const int row = row0 + min(32 * wave + i32, rows - 1), token = row / a.group, limit = p.length - p.n + token;
+        const bool some = 32 * wave < rows;
+        const int w_last = row0 + min(32 * wave + 31, rows - 1);
+        const int sees_first = p.length - p.n + (row0 + 32 * wave) / a.group, sees_last = some ? p.length - p.n + w_last / a.group : -1;
+        const int seen = p.length - p.n + (row0 + rows - 1) / a.group + 1;       // keys that any of the rows sees
+        const int full = p.length / kBlock, tail = p.length - full * kBlock;
+        const int blocks = min(full, (max(seen, 0) + kBlock - 1) / kBlock);      // in pages
+        const bool has_tail = tail > 0 && seen > full * kBlock;
+        const int done = min(last, (blocks + (has_tail ? 1 : 0) + kStageBlocks - 1) / kStageBlocks);
+        const uint16_t *recent = B::recent(c, p.id, head);
+        v8h q[D / 16];
+        {
+            const uint16_t *from = a.q + (size_t)(p.begin + token) * a.q_stride + (size_t)(head * a.group + row - token * a.group) * D;
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 16 * m + 8 * half);
         }
-        store_row(a, p.begin, p.tile * ROWS + row, head, D, d, o, l);
+        v4u k_codes[TASKS], v_codes[TASKS];
+        // lane b, b = 0 .. 3: the table's entry and the scales of block b of a stage (0: the block is not there)
+        int pages = -1;
+        unsigned scales = 0u;
+        const int mine = lane & (kStageBlocks - 1);
+        // planes of a stage: number n of a wavefront is plane n + TASKS wave, plane j of block b being D / 64 b + j
+        auto block_of = [&](int n) { return (TASKS * wave + n) / (D / 64); };
+        auto ask_pages = [&](int s) {
+            if (blocks > 0) pages = c.table[(size_t)p.id * c.max_pages + (min(kStageBlocks * s + mine, blocks - 1) >> c.shift)];
+        };
+        auto fetch = [&](int s) {                    // (after ask_pages of the same stage)
+            const bool there = pages >= 0 && pages < c.pages && kStageBlocks * s + mine < blocks;
+            const int good = pages >= 0 && pages < c.pages ? pages : 0;
+#pragma unroll
+            for (int n = 0; n < TASKS; ++n) {
+                const int block = min(kStageBlocks * s + block_of(n), max(blocks - 1, 0)), plane = (TASKS * wave + n) % (D / 64);
+                const uint8_t *codes = B::codes(c, __builtin_amdgcn_readlane(good, block_of(n)), head, block);
+                k_codes[n] = reinterpret_cast<const v4u *>(codes + 1024 * plane)[lane];
+                v_codes[n] = reinterpret_cast<const v4u *>(codes + kBlock * D + 1024 * plane)[lane];
+            }
+            scales = *B::scales(c, good, head, there ? kStageBlocks * s + mine : 0);
+            if (!there) scales = 0u;
+        };
+        auto put = [&](int s) {
+            uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
+            const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+            for (int n = 0; n < TASKS; ++n) {
+                const int b = block_of(n), plane = (TASKS * wave + n) % (D / 64), line = kBlock * b + i;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<v8h *>(ks + line * LINE + 16 * ((8 * plane + 4 * h + g) ^ key_swizzle(line))) =
+                        codes_to_half(k_codes[n][2 * h], k_codes[n][2 * h + 1]);
+#pragma unroll
+                for (int t = 0; t < 4; t += 2) {
+                    union {
+                        v8h v;
+                        v2u u[2];
+                    } w;
+                    w.v = codes_to_half(v_codes[n][t], v_codes[n][t + 1]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int channel = 64 * plane + 16 * (t + h) + i;
+                        *reinterpret_cast<v2u *>(vs + channel * 128 + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) = w.u[h];
+                    }
+                }
+            }
+        };
+        // the unfinished block's tokens over what was put in its place
+        auto put_tail = [&](int s) {
+            uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
+            const int b = full - kStageBlocks * s;
+            for (int u = threadIdx.x; u < kBlock * (D / 8); u += 64 * kStageWaves) {
+                const int t = u / (D / 8), chunk = u % (D / 8), line = kBlock * b + t;
+                v4u w = {0u, 0u, 0u, 0u};
+                if (recent && t < tail) w = *reinterpret_cast<const v4u *>(recent + B::recent_key(full * kBlock + t, 8 * chunk));
+                *reinterpret_cast<v4u *>(ks + line * LINE + 16 * (chunk ^ key_swizzle(line))) = w;
+            }
+            for (int u = threadIdx.x; u < 4 * D; u += 64 * kStageWaves) {
+                const int g = u & 3, channel = u >> 2;
+                uint16_t w[4] = {0, 0, 0, 0};        // (behind the last token anything may lie)
+                if (recent) {
+                    const uint16_t *from = recent + B::recent_value(full * kBlock + 4 * g, channel);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (4 * g + e < tail) w[e] = from[e];
+                }
+                *reinterpret_cast<v2u *>(vs + channel * 128 + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) =
+                    v2u{(unsigned)w[0] | ((unsigned)w[1] << 16), (unsigned)w[2] | ((unsigned)w[3] << 16)};
+            }
+        };
+        v16f o[D / 32];
+        float top = kNothing, sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        auto prepare = [&](int s) {                  // stage s, asked for, into its buffer
+            put(s);
+            if (has_tail && full / kStageBlocks == s) {
+                __syncthreads();
+                put_tail(s);
+            }
+        };
+        __syncthreads();                             // (the tile before is done with the buffers)
+        if (first < done) {
+            ask_pages(first);
+            fetch(first);
+            ask_pages(first + 1);
+            prepare(first);
+        }
+        for (int s = first; s < done; ++s) {
+            const unsigned sc = scales;
+            __syncthreads();                         // the stage is there, and everyone is done with the one before
+            if (s + 1 < done) {
+                fetch(s + 1);
+                ask_pages(s + 2);
+            }
+            if (some && kStageKeys * s <= sees_last) {
+                const uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
+                v16f x[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int line = 32 * u + i32;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[u][i] = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m)
+                        x[u] = mfma_h(*reinterpret_cast<const v8h *>(ks + line * LINE + 16 * ((2 * m + half) ^ key_swizzle(line))), q[m], x[u]);
+                }
+                // the blocks' scales: of keys, with the call's; of values, their logarithm and what takes it back
+                float scale[kStageBlocks], lv[kStageBlocks], back[kStageBlocks];
+                {
+                    const bool code = sc != 0u, ring = has_tail && recent && kStageBlocks * s + mine == full;
+                    const float k = code ? h2f((uint16_t)(sc & 0xffffu)) * a.scale : a.scale;
+                    const float v = code ? __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16))) : ring ? 0.0f : -INFINITY;
+                    const float inv = code || ring ? __builtin_amdgcn_exp2f(-v) : 0.0f;
+#pragma unroll
+                    for (int b = 0; b < kStageBlocks; ++b) {
+                        scale[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k), b));
+                        lv[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), b));
+                        back[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(inv), b));
+                    }
+                }
+                if (kStageKeys * (s + 1) - 1 > sees_first) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (kStageKeys * s + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3) > limit) x[u][i] = -INFINITY;
+                }
+                v8h w[2][2];
+                float part[kStageBlocks];
+                auto weights = [&] {
+#pragma unroll
+                    for (int b = 0; b < kStageBlocks; ++b) {
+                        const float less = top - kStageShift - lv[b];
+                        part[b] = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 8; i += 2) {
+                            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b / 2][8 * (b & 1) + i], scale[b], -less));
+                            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b / 2][8 * (b & 1) + i + 1], scale[b], -less));
+                            part[b] += e0;
+                            part[b] += e1;
+                            const v2h h = __builtin_convertvector((v2f{e0, e1}), v2h);
+                            w[b / 2][b & 1][i] = h[0];
+                            w[b / 2][b & 1][i + 1] = h[1];
+                        }
+                    }
+                };
+                weights();
+                if (__any(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) > kMost)) {
+                    float best = kNothing;
+#pragma unroll
+                    for (int b = 0; b < kStageBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) best = fmaxf(best, x[b / 2][8 * (b & 1) + i] * scale[b] + lv[b]);
+                    auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+                    const float next = fmaxf(top, fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+                    const float f = __builtin_amdgcn_exp2f(top - next);
+                    top = next;
+                    sum *= f;
+#pragma unroll
+                    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[t][i] *= f;
+                    weights();
+                }
+                sum += (part[0] * back[0] + part[1] * back[1]) + (part[2] * back[2] + part[3] * back[3]);
+#pragma unroll
+                for (int b = 0; b < kStageBlocks; ++b)
+#pragma unroll
+                    for (int t = 0; t < D / 32; ++t) {
+                        const int channel = 32 * t + i32;
+                        o[t] = mfma_h(*reinterpret_cast<const v8h *>(vs + channel * 128 + 16 * ((2 * b + half) ^ value_swizzle(channel))),
+                                      w[b / 2][b & 1], o[t]);
+                    }
+            }
+            if (s + 1 < done) prepare(s + 1);
+        }
+        {
+            auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+            sum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+        }
+        if (32 * wave + i32 < rows) {
+            float *part = a.part + ((((size_t)head * a.parts + index) * 2 + (first == 0 ? 1 : 0)) * kStageRows + 32 * wave + i32) * (D + 4);
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = 32 * t + 8 * i + 4 * half;
+                    const v4f y = {o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+                    if (whole)
+                        store_row(a, p.begin, row, head, D, d, y, sum);
+                    else
+                        *reinterpret_cast<v4f *>(part + d) = y;
+                }
+            if (!whole && half == 0) {
+                part[D] = top;
+                part[D + 1] = sum;
+            }
+        }
+        at = end;
     }
+}
+
+// Tiles that several workgroups took: their shares in order.  Wavefront (i, group) has some rows, one after the other, of
+// the tile that begins in part i and does not end there, if there is one: with many rows 256 / D of them, a row of few shares
+// each; with few rows one, whose shares its lanes take in turn.
+template <int D, int ROWS, int KEYS>
+__global__ __launch_bounds__(64) void join_kernel(CachedArgs a, int groups)
+{
+    constexpr int Q = D / 4, SHARES = ROWS == kStageRows ? 1 : 64 / Q, HIGH = 64 / Q / SHARES, U = 8;    // Q: lanes of a row
+    __shared__ __attribute__((aligned(16))) float red[SHARES][D];
+    __shared__ float stat[SHARES][2];
+    const CacheArgs &c = a.c;
+    const int head = blockIdx.x % c.kv_heads, group = blockIdx.x / c.kv_heads % groups, index = blockIdx.x / c.kv_heads / groups;
+    Steps<ROWS, KEYS> all(a);
+    const int total = all.all(), width = part_width(a, total);
+    const int start = index * width, stop = start + width;
+    if (stop >= total) return;
+    const Place p = all.find(stop);
+    if (p.id < 0 || p.first >= stop || p.first < start) return;
+    const int rows = p.n * a.group - p.tile * ROWS;
+    const int d = threadIdx.x % Q * 4, share = SHARES == 1 ? 0 : threadIdx.x / Q;
+    const int row = SHARES == 1 ? HIGH * group + threadIdx.x / Q : group;
+    if (HIGH * group >= rows) return;
+    const int last = (p.first + p.steps - 1) / width;            // the last part that has some of the tile
+    const float *part = a.part + (((size_t)head * a.parts) * 2 * ROWS + min(row, rows - 1)) * (D + 4);
+    auto of = [&](int i) { return part + ((size_t)i * 2 + (i == index ? 1 : 0)) * ROWS * (D + 4); };
+    float m = kNothing, l = 0.0f;
+    v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](float mi, float li, v4f oi) {
+        const float top = fmaxf(m, mi), f = __builtin_amdgcn_exp2f(m - top), fi = __builtin_amdgcn_exp2f(mi - top);
+        m = top;
+        l = l * f + li * fi;
+        o = o * f + oi * fi;
+    };
+    for (int i = index + share; i <= last; i += U * SHARES) {    // (U loads set out together)
+        float mi[U], li[U];
+        v4f oi[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float *from = of(min(i + u * SHARES, last));
+            oi[u] = *reinterpret_cast<const v4f *>(from + d);
+            mi[u] = from[D];
+            li[u] = from[D + 1];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u * SHARES <= last) add(mi[u], li[u], oi[u]);
+    }
+    if (SHARES > 1) {
+        stat[share][0] = m;                                      // (every lane of a share writes the same)
+        stat[share][1] = l;
+        *reinterpret_cast<v4f *>(&red[share][d]) = o;
+        __syncthreads();
+        if (share != 0) return;
+#pragma unroll
+        for (int i = 1; i < SHARES; ++i) add(stat[i][0], stat[i][1], *reinterpret_cast<const v4f *>(&red[i][d]));
+    }
+    if (row < rows) store_row(a, p.begin, p.tile * ROWS + row, head, D, d, o, l);
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Workgroups of a launch: about four a CU.
-int parts_for(int kv_heads)
-{
-    const int parts = 1024 / kv_heads;
-    return parts < 1 ? 1 : parts;
-}
-
-// Rows of a tile, by 16: as many as a sequence has on average.
-int row_blocks(int M, int count, int group)
+// Rows of a tile: as many as a sequence has on average.
+int tile_rows(int M, int count, int group)
 {
     const long rows = (long)M * group / count;
-    return rows >= 48 ? 4 : rows >= 24 ? 2 : 1;
+    return rows >= 64 ? kStageRows : rows >= 24 ? 32 : 16;
+}
+
+// Workgroups of a key head: one a CU in all of the streaming kernel, two of the other.
+int parts_for(int kv_heads, int rows)
+{
+    const int parts = (rows == kStageRows ? 512 : 256) / kv_heads;
+    return parts < 1 ? 1 : parts;
 }
 
 size_t workspace_for(int M, int count, int heads, int kv_heads, int head_dim)
 {
-    return (size_t)parts_for(kv_heads) * kv_heads * 2 * 16 * row_blocks(M, count, heads / kv_heads) * (head_dim + 4) * 4;
+    const int rows = tile_rows(M, count, heads / kv_heads);
+    return (size_t)parts_for(kv_heads, rows) * kv_heads * 2 * rows * (head_dim + 4) * 4;
 }
 
 }  // namespace
@@ -483,7 +801,9 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     if (heads < 1 || heads % kv != 0 || !(scale > 0.0f && scale <= 65504.0f)) return FLEXQ_EINVAL;
     if ((long)heads * D > FLEXQ_MAX_K || q_stride < heads * D || out_stride < heads * D || q_stride % 8 != 0 || out_stride % 8 != 0)
         return FLEXQ_ESHAPE;
-    if ((long)M * (heads / kv) >= (1L << 30)) return FLEXQ_ESHAPE;
+    // (steps are counted with 32 bits)
+    const long tiles = (long)M * (heads / kv) / 16 + seqs->count, steps = (long)seqs->max_pages * cache->page / (2 * kBlock) + 1;
+    if ((long)M * (heads / kv) >= (1L << 30) || tiles * steps >= (1L << 31)) return FLEXQ_ESHAPE;
     if (!aligned16(q) || !aligned16(out)) return FLEXQ_EALIGN;
     if (!workspace || workspace_bytes < workspace_for(M, seqs->count, heads, kv, D)) return FLEXQ_EWORKSPACE;
     if (!aligned16(workspace)) return FLEXQ_EALIGN;
@@ -495,25 +815,25 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     a.scale = scale * 1.44269504088896341f;
     a.group = heads / kv;
     a.heads = heads;
-    a.parts = parts_for(kv);
-    a.least = 8;
-    const int rb = row_blocks(M, seqs->count, a.group);
-    const int rows = (long)M * a.group < 16 * rb ? M * a.group : 16 * rb, per = 256 / (D / 4);
-    const int slices = (rows + per - 1) / per;
+    const int rows = tile_rows(M, seqs->count, a.group), most = (long)M * a.group < rows ? M * a.group : rows;
+    a.parts = parts_for(kv, rows);
+    a.least = rows == kStageRows ? 4 : 8;
+    const int groups = rows == kStageRows ? (most + 256 / D - 1) / (256 / D) : most;     // of rows of a tile
+    if ((long)a.parts * kv * groups >= (1L << 26)) return FLEXQ_ESHAPE;  // 64 threads each, 2^32 a launch
     hipStream_t st = (hipStream_t)stream;
-    auto run = [&](auto kern, auto join) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)(a.parts * kv)), dim3(64 * kWaves), 0, st, a);
+    auto run = [&](auto kern, int waves, auto join) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)(a.parts * kv)), dim3(64 * waves), 0, st, a);
         if (hipGetLastError() != hipSuccess) return FLEXQ_EHIP;
-        if (a.parts > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.parts * kv * slices)), dim3(256), 0, st, a, slices);
+        if (a.parts > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.parts * kv * groups)), dim3(64), 0, st, a, groups);
         return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
     };
     if (D == 128)
-        return rb == 4   ? run(cached_kernel<128, 4>, join_kernel<128, 4>)
-               : rb == 2 ? run(cached_kernel<128, 2>, join_kernel<128, 2>)
-                         : run(cached_kernel<128, 1>, join_kernel<128, 1>);
-    return rb == 4   ? run(cached_kernel<64, 4>, join_kernel<64, 4>)
-           : rb == 2 ? run(cached_kernel<64, 2>, join_kernel<64, 2>)
-                     : run(cached_kernel<64, 1>, join_kernel<64, 1>);
+        return rows == kStageRows ? run(chunk_kernel<128>, kStageWaves, join_kernel<128, kStageRows, kStageKeys>)
+               : rows == 32       ? run(cached_kernel<128, 2>, kWaves, join_kernel<128, 32, 2 * kBlock>)
+                                  : run(cached_kernel<128, 1>, kWaves, join_kernel<128, 16, 2 * kBlock>);
+    return rows == kStageRows ? run(chunk_kernel<64>, kStageWaves, join_kernel<64, kStageRows, kStageKeys>)
+           : rows == 32       ? run(cached_kernel<64, 2>, kWaves, join_kernel<64, 32, 2 * kBlock>)
+                              : run(cached_kernel<64, 1>, kWaves, join_kernel<64, 16, 2 * kBlock>);
 }
 
 }  // extern "C"

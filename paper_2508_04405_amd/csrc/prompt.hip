@@ -4,14 +4,22 @@
 //
 // Rows of a tile are the tokens of a sequence times the heads that share a key head, 32 a wavefront, so that grouped heads
 // share the keys a workgroup stages and a short prompt fills a tile.  Keys and values come 64 at a time into LDS (direct
-// loads, two buffers, chunks of 16 bytes swizzled by the row); rows past the sequence's end read as zero.  S^T = K Q^T by
-// 32x32x16 MFMAs: a lane holds 32 scores of one row, its other half lane l ^ 32, so that the running maximum is one exchange and
-// everything else stays in the lane.  Its scores in the order of the registers are the column operand of O^T = V^T P^T for
-// keys {0..3, 8..11} + 4 (l / 32) of every sixteen; the row operand is read from LDS transposed, in that order of keys.
+// loads, two buffers).  S^T = K Q^T by 32x32x16 MFMAs: a lane holds 32 scores of one row, lane l ^ 32 the row's other 32.  Its
+// scores in the order of the registers are the column operand of O^T = V^T P^T for keys {0..3, 8..11} + 4 (l / 32) of every
+// sixteen; the row operand is read from LDS transposed, in that order of keys, so that weights never cross lanes.
 //
-// p enters the MFMA in fp16 times 2^9 and the running maximum is only raised once a score passes it by 6 (powers of two): p
-// is at most 2^15 there and normal down to 2^-23 of that, and the output is rarely rescaled.  The sum of p is fp32,
-// unrounded.
+// The maximum that is taken off a score, m, is not the running one but one it was at some time: p = 2^(x - m + 9), and as long as a
+// lane's 32 of a stage add up to 2^15 at most -- which the running sum needs anyway -- nothing overflows in fp16.  Where they
+// do not (at the first stage, and rarely after it) m becomes the running maximum, and what was added up is scaled down.  So the
+// maximum of each stage, a quarter of its vector instructions, is not taken.  p is normal down to 2^-23 of the largest;
+// its sum is fp32, unrounded.
+//
+// What bounds it: power.  16384 tokens of 64 heads over 8 take 4.2 ms, 1.05 PFLOP/s (of what the mask leaves; PyTorch's
+// fp16 product of 8192^3 reaches 1.14), the matrix pipe busy 53 % of the cycles at 1.9 GHz.  A form that interleaves exponentials
+// with matrix instructions, one block's beside the next one's scores, took 12 % fewer cycles, but at 1.76 GHz, for 1 % of the
+// time; without any load of keys and values, at 1.6 GHz, it would take 3.65 ms.  Operands of S four reads ahead of the
+// instruction that takes them: 4.31 -> 4.2.  4 wavefronts instead of 8: 4.28, but two workgroups a CU, and so better
+// below some thousand tokens (1024 tokens 32 -> 37 us, packed prompts of 300 37 -> 49 with 8).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
@@ -23,7 +31,7 @@ namespace {
 
 constexpr int kKeys = 64;                        // of a stage
 constexpr float kNothing = -1e30f;
-constexpr float kShift = 9.0f, kLag = 6.0f;
+constexpr float kShift = 9.0f, kMost = 32768.0f;
 
 struct PromptArgs {
     const uint16_t *q, *k, *v;
@@ -52,14 +60,27 @@ __device__ __forceinline__ v4h read_transposed(const uint8_t *at)
     return x.h;
 }
 
+// Which chunk of 16 bytes of a staged row lies where: XOR by the row, so that a cycle's lanes (256 bytes) meet every bank
+// once -- sixteen keys' same chunk; 32 channels of four keys, read transposed.
+template <int D>
+__device__ __forceinline__ int key_swizzle(int line)
+{
+    return D == 128 ? line & 15 : (line >> 1) & 7;
+}
+template <int D>
+__device__ __forceinline__ int value_swizzle(int line)
+{
+    return D == 128 ? 4 * (line & 3) : 4 * ((line >> 1) & 1);
+}
+
 template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void prompt_kernel(PromptArgs a)
 {
     constexpr int ROWS = 32 * WAVES, LINE = 2 * D, CH = D / 8;           // LINE: bytes of a staged row; CH: its chunks
     constexpr int STAGE = kKeys * LINE, DMA = STAGE / 1024 / WAVES;      // DMA: loads of a wavefront for keys, or values
     static_assert(STAGE % (1024 * WAVES) == 0, "a stage is whole loads of every wavefront");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][STAGE];  // [buffer][keys, values]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, i32 = lane & 31;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
     const int head = blockIdx.x % a.kv_heads;
     const int pieces = gridDim.x / a.kv_heads;
     // the tiles with most keys first
@@ -83,33 +104,36 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
         for (int m = 0; m < D / 16; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 16 * m);
     }
     // stages: load i of a wavefront fills 1 KiB, lane l 16 bytes at 16 l, and so fetches the chunk that the swizzle keeps there
-    int s_row[DMA], k_chunk[DMA], v_chunk[DMA];
-#pragma unroll
-    for (int i = 0; i < DMA; ++i) {
-        const int at = (wave * DMA + i) * 64 + lane, line = at / CH, c = at % CH;
-        s_row[i] = line;
-        k_chunk[i] = c ^ (D == 128 ? line & 15 : (line >> 1) & 7);
-        v_chunk[i] = c ^ (D == 128 ? 2 * (line & 7) : 2 * (line & 3));
-    }
+    // rows past the sequence's end repeat its last one: they are hidden, and p = 0 meets finite values
     const uint16_t *k0 = a.k + (size_t)r.begin * a.k_stride + (size_t)head * D;
     const uint16_t *v0 = a.v + (size_t)r.begin * a.v_stride + (size_t)head * D;
+    unsigned k_from[DMA], v_from[DMA];               // of whole stages
+    auto from = [&](int i, int most, unsigned line_bytes, bool values) {
+        const int at = (wave * DMA + i) * 64 + lane, line = at / CH, swizzle = values ? value_swizzle<D>(line) : key_swizzle<D>(line);
+        return (unsigned)min(line, most) * line_bytes + 16u * (unsigned)(at % CH ^ swizzle);
+    };
+    const unsigned k_line = 2 * (unsigned)a.k_stride, v_line = 2 * (unsigned)a.v_stride;
+#pragma unroll
+    for (int i = 0; i < DMA; ++i) {
+        k_from[i] = from(i, kKeys, k_line, false);
+        v_from[i] = from(i, kKeys, v_line, true);
+    }
     auto fetch = [&](int stage, int buf) {
-        const int left = min(kKeys, r.n - stage * kKeys);                // rows of the sequence there are
-        const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)(k0 + (size_t)stage * kKeys * a.k_stride), 0, (unsigned)((left - 1) * (int)a.k_stride * 2 + LINE), 0x00020000);
-        const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
-            (void *)(v0 + (size_t)stage * kKeys * a.v_stride), 0, (unsigned)((left - 1) * (int)a.v_stride * 2 + LINE), 0x00020000);
-        const unsigned beyond = 0x7fffffffu;                             // of any stage's rows: reads as zero
+        const int most = min(kKeys, r.n - stage * kKeys) - 1;
+        const __amdgpu_buffer_rsrc_t kr =
+            __builtin_amdgcn_make_buffer_rsrc((void *)(k0 + (size_t)stage * kKeys * a.k_stride), 0, (unsigned)most * k_line + LINE, 0x00020000);
+        const __amdgpu_buffer_rsrc_t vr =
+            __builtin_amdgcn_make_buffer_rsrc((void *)(v0 + (size_t)stage * kKeys * a.v_stride), 0, (unsigned)most * v_line + LINE, 0x00020000);
 #pragma unroll
         for (int i = 0; i < DMA; ++i) {
             uint8_t *dst = &lds[buf][0][(wave * DMA + i) * 1024];
-            const unsigned off = s_row[i] < left ? (unsigned)(s_row[i] * (int)a.k_stride * 2 + 16 * k_chunk[i]) : beyond;
+            const unsigned off = most == kKeys - 1 ? k_from[i] : from(i, most, k_line, false);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (void __attribute__((address_space(3))) *)dst, 16, off, 0, 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < DMA; ++i) {
             uint8_t *dst = &lds[buf][1][(wave * DMA + i) * 1024];
-            const unsigned off = s_row[i] < left ? (unsigned)(s_row[i] * (int)a.v_stride * 2 + 16 * v_chunk[i]) : beyond;
+            const unsigned off = most == kKeys - 1 ? v_from[i] : from(i, most, v_line, true);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (void __attribute__((address_space(3))) *)dst, 16, off, 0, 0, 0);
         }
     };
@@ -129,15 +153,24 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
         if (first > sees_any) continue;
         const uint8_t *ks = lds[buf][0], *vs = lds[buf][1];
         v16f s[2];
+        {
+            constexpr int AHEAD = 4;                 // operands asked for ahead of the instruction that takes them
+            v8h ring[AHEAD];
+            auto key_part = [&](int n) {             // n: block n % 2, channels 16 (n / 2) ..
+                const int line = 32 * (n & 1) + i32;
+                return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * (((n & ~1) + half) ^ key_swizzle<D>(line)));
+            };
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+            for (int n = 0; n < AHEAD; ++n) ring[n] = key_part(n);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int m = 0; m < D / 16; ++m) {
-                const int line = 32 * b + i32;
-                const int c = (2 * m + half) ^ (D == 128 ? line & 15 : (line >> 1) & 7);
-                s[b] = mfma_h(*reinterpret_cast<const v8h *>(ks + line * LINE + 16 * c), q[m], s[b]);
+                for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+                s[n & 1] = mfma_h(ring[n % AHEAD], q[n >> 1], s[n & 1]);
+                if (n + AHEAD < D / 8) ring[n % AHEAD] = key_part(n + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (first + kKeys - 1 > sees_all) {
@@ -147,44 +180,43 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
                 for (int i = 0; i < 16; ++i)
                     if (first + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) > token) s[b][i] = -INFINITY;
         }
-        float best = s[0][0];
+        v8h p[2][2];
+        float part;
+        auto weights = [&] {
+            const float less = top - kShift;
+            part = 0.0f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) best = fmaxf(best, s[0][i]);
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) best = fmaxf(best, s[1][i]);
-        {
-            auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
-            best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * a.scale;
-        }
-        if (__any(best > top + kLag)) {
-            const float next = fmaxf(top, best), f = __builtin_amdgcn_exp2f(top - next);
+                for (int i = 0; i < 16; i += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale, -less));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i + 1], a.scale, -less));
+                    part += e0;
+                    part += e1;
+                    const v2h h = __builtin_convertvector((v2f{e0, e1}), v2h);
+                    p[b][i / 8][i % 8] = h[0];
+                    p[b][i / 8][i % 8 + 1] = h[1];
+                }
+        };
+        weights();
+        if (__any(part > kMost)) {                   // a score far above m
+            float x = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) x = fmaxf(x, s[0][i]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = fmaxf(x, s[1][i]);
+            auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+            const float next = fmaxf(top, fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * a.scale);
+            const float f = __builtin_amdgcn_exp2f(top - next);
             top = next;
             sum *= f;
 #pragma unroll
             for (int t = 0; t < D / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[t][i] *= f;
+            weights();
         }
-        const float less = top - kShift;
-        v8h p[2][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                union {
-                    v2h h[4];
-                    v8h v;
-                } x;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * u + 2 * i], a.scale, -less));
-                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * u + 2 * i + 1], a.scale, -less));
-                    sum += e0;
-                    sum += e1;
-                    x.h[i] = __builtin_convertvector((v2f{e0, e1}), v2h);
-                }
-                p[b][u] = x.v;
-            }
+        sum += part;
         // lane (dsub, h) of sixteen lanes each: keys 4 h + 0 .. 3 (and 8 more on) of channels 16 dsub .. + 15
         const int h = lane >> 5, dsub = lane >> 4 & 1, e = lane >> 2 & 3, c4 = lane & 3;
 #pragma unroll
@@ -200,7 +232,7 @@ __global__ __launch_bounds__(64 * WAVES) void prompt_kernel(PromptArgs a)
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
                         const int line = 32 * b + 16 * u + 8 * w + 4 * h + e;
-                        const int c = (4 * t + 2 * dsub + (c4 >> 1)) ^ (D == 128 ? 2 * (line & 7) : 2 * (line & 3));
+                        const int c = (4 * t + 2 * dsub + (c4 >> 1)) ^ value_swizzle<D>(line);
                         x.h[w] = read_transposed(vs + line * LINE + 16 * c + 8 * (c4 & 1));
                     }
                     o[t] = mfma_h(x.v, p[b][u], o[t]);
@@ -258,13 +290,16 @@ flexq_status flexq_prompt_attention(const uint16_t *q, int q_stride, const uint1
     a.kv_heads = kv_heads;
     a.scale = scale * 1.44269504088896341f;
     if ((long)M * a.group >= (1L << 30)) return FLEXQ_ESHAPE;
-    constexpr int waves = 4;
+    // 256 rows a workgroup instead of 128 where they fill the chip four times over, and heads are of 128 (us with 128 / 256
+    // rows: 16384 tokens of 64 heads over 8 4280 / 4200, 8192 of 32 543 / 533, 4096 of 64 over 8 287 / 289; heads of 64, 16384
+    // of 24 over 6, 873 / 940)
+    const int waves = head_dim == 128 && (long)M * a.group / 256 * kv_heads >= 1024 ? 8 : 4;
     const long grid = ((long)M * a.group / (32 * waves) + sequences) * kv_heads;
     if (grid * 64 * waves >= (1L << 32)) return FLEXQ_ESHAPE;            // threads of a launch
     auto launch = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * waves), 0, (hipStream_t)stream, a);
     };
-    head_dim == 128 ? launch(prompt_kernel<128, waves>) : launch(prompt_kernel<64, waves>);
+    head_dim == 64 ? launch(prompt_kernel<64, 4>) : waves == 4 ? launch(prompt_kernel<128, 4>) : launch(prompt_kernel<128, 8>);
     return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
 }
 
