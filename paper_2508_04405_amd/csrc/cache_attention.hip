@@ -492,18 +492,20 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
             for (int m = 0; m < D / 16; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 16 * m + 8 * half);
         }
         v4u k_codes[TASKS], v_codes[TASKS];
-        // lane b, b = 0 .. 3: the table's entry and the scales of block b of a stage (0: the block is not there)
+        // lane b, b = 0 .. 3: the table's entry and the scales of block b of a stage, and whether the block is there
         int pages = -1;
         unsigned scales = 0u;
+        bool there = false;
         const int mine = lane & (kStageBlocks - 1);
         // planes of a stage: number n of a wavefront is plane n + TASKS wave, plane j of block b being D / 64 b + j
         auto block_of = [&](int n) { return (TASKS * wave + n) / (D / 64); };
         auto ask_pages = [&](int s) {
-            if (blocks > 0) pages = c.table[(size_t)p.id * c.max_pages + (min(kStageBlocks * s + mine, blocks - 1) >> c.shift)];
+            pages = c.table[(size_t)p.id * c.max_pages + (max(min(kStageBlocks * s + mine, blocks - 1), 0) >> c.shift)];
         };
         auto fetch = [&](int s) {                    // (after ask_pages of the same stage)
-            const bool there = pages >= 0 && pages < c.pages && kStageBlocks * s + mine < blocks;
-            const int good = pages >= 0 && pages < c.pages ? pages : 0;
+            const bool valid = pages >= 0 && pages < c.pages;
+            const int good = valid ? pages : 0;
+            there = valid && kStageBlocks * s + mine < blocks;
 #pragma unroll
             for (int n = 0; n < TASKS; ++n) {
                 const int block = min(kStageBlocks * s + block_of(n), max(blocks - 1, 0)), plane = (TASKS * wave + n) % (D / 64);
@@ -512,7 +514,6 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                 v_codes[n] = reinterpret_cast<const v4u *>(codes + kBlock * D + 1024 * plane)[lane];
             }
             scales = *B::scales(c, good, head, there ? kStageBlocks * s + mine : 0);
-            if (!there) scales = 0u;
         };
         auto put = [&](int s) {
             uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
@@ -582,8 +583,10 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
             ask_pages(first + 1);
             prepare(first);
         }
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) asm volatile("" : "+v"(q[m]));  // (they are waited for here, not in the loop)
         for (int s = first; s < done; ++s) {
-            const unsigned sc = scales;
+            const unsigned sc = there ? scales : 0u;
             __syncthreads();                         // the stage is there, and everyone is done with the one before
             if (s + 1 < done) {
                 fetch(s + 1);
@@ -592,14 +595,25 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
             if (some && kStageKeys * s <= sees_last) {
                 const uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
                 v16f x[2];
+                {
+                    constexpr int AHEAD = 4;         // operands asked for ahead of the instruction that takes them
+                    v8h ring[AHEAD];
+                    auto key_part = [&](int n) {     // n: keys 32 (n % 2) .., channels 16 (n / 2) ..
+                        const int line = 32 * (n & 1) + i32;
+                        return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * (((n & ~1) + half) ^ key_swizzle(line)));
+                    };
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int line = 32 * u + i32;
+                    for (int n = 0; n < AHEAD; ++n) ring[n] = key_part(n);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[u][i] = 0.0f;
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int m = 0; m < D / 16; ++m)
-                        x[u] = mfma_h(*reinterpret_cast<const v8h *>(ks + line * LINE + 16 * ((2 * m + half) ^ key_swizzle(line))), q[m], x[u]);
+                        for (int i = 0; i < 16; ++i) x[u][i] = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < D / 8; ++n) {
+                        x[n & 1] = mfma_h(ring[n % AHEAD], q[n >> 1], x[n & 1]);
+                        if (n + AHEAD < D / 8) ring[n % AHEAD] = key_part(n + AHEAD);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
                 // the blocks' scales: of keys, with the call's; of values, their logarithm and what takes it back
                 float scale[kStageBlocks], lv[kStageBlocks], back[kStageBlocks];
@@ -757,11 +771,13 @@ __global__ __launch_bounds__(64) void join_kernel(CachedArgs a, int groups)
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Rows of a tile: as many as a sequence has on average.
+// Rows of a tile: as many as a sequence has on average; 128, which go through LDS, from 65 on, where tiles of 32 would read
+// the cache three times (us with 32 / 128 a tile: 64 rows, 16 sequences of 1000 tokens of 8 key heads 21.8 / 34, of 4000 46 / 60;
+// 65 rows, 40 of 2000 of 6 heads of 64 61 / 43; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
 int tile_rows(int M, int count, int group)
 {
     const long rows = (long)M * group / count;
-    return rows >= 64 ? kStageRows : rows >= 24 ? 32 : 16;
+    return rows > 64 ? kStageRows : rows > 16 ? 32 : 16;
 }
 
 // Workgroups of a key head: one a CU in all of the streaming kernel, two of the other.
