@@ -44,11 +44,13 @@ __device__ __forceinline__ unsigned code4(const uint16_t (&h)[4], float s, float
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+__global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs a)
 {
     typedef CacheBlock<D> B;
-    constexpr int KEYS = kBlock * D / 8;                 // threads with eight elements of a key
-    __shared__ unsigned top[2][4];
+    // the first half of the threads takes values, four tokens of four channels each, the other keys, two times eight elements
+    constexpr int THREADS = 2 * D, WAVES = D / 64;               // WAVES: of either half
+    __shared__ unsigned top[2 * WAVES];
+    __shared__ __attribute__((aligned(16))) uint8_t block[B::kBytes];    // the block's codes as they go out, 16 bytes a thread
     const CacheArgs &c = a.c;
     const int tid = threadIdx.x, head = blockIdx.x % c.kv_heads;
     const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, blockIdx.x / c.kv_heads);
@@ -62,65 +64,73 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     auto row = [&](int token) { return (size_t)(r.begin + (token - first)); };
     if (b < full) {
         const int page = B::page_of(c, r.id, b);
-        const int token = tid / (D / 8), d = tid % (D / 8) * 8;              // a key's elements of this thread
-        const int quad = tid / (D / 2), dv = tid % (D / 2) * 2;              // four tokens' values of two channels
-        uint4 kv = make_uint4(0u, 0u, 0u, 0u);
-        unsigned vv[4] = {0u, 0u, 0u, 0u};
-        if (page >= 0) {
-            if (KEYS == 256 || tid < KEYS) {
-                const int t = b * kBlock + token;
-                if (t >= first)
-                    kv = *reinterpret_cast<const uint4 *>(k + row(t) * a.k_stride + d);
-                else if (recent)
-                    kv = *reinterpret_cast<const uint4 *>(recent + B::recent_key(t, d));
-            }
-            if (D == 128 || quad < 4) {
+        const bool values = tid < D;
+        const int quad = tid / (D / 4), dv = tid % (D / 4) * 4;              // values: tokens 4 quad .., channels dv ..
+        const int token = (tid - D) / (D / 8), dk = tid % (D / 8) * 8;       // keys: tokens token and token + 8, elements dk ..
+        uint2 vv[4];
+        uint4 kv[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = b * kBlock + 4 * quad + i;
-                    if (t >= first)
-                        vv[i] = *reinterpret_cast<const unsigned *>(v + row(t) * a.v_stride + dv);
-                    else if (recent)
-                        vv[i] = recent[B::recent_value(t, dv)] | ((unsigned)recent[B::recent_value(t, dv + 1)] << 16);
-                }
+        for (int i = 0; i < 4; ++i) vv[i] = make_uint2(0u, 0u);
+        kv[0] = kv[1] = make_uint4(0u, 0u, 0u, 0u);
+        // (whether the block has a page is not waited for: the table is read while the rows are)
+        if (values) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = b * kBlock + 4 * quad + i;
+                if (t >= first)
+                    vv[i] = *reinterpret_cast<const uint2 *>(v + row(t) * a.v_stride + dv);
+                else if (recent)
+                    vv[i] = make_uint2(recent[B::recent_value(t, dv)] | ((unsigned)recent[B::recent_value(t, dv + 1)] << 16),
+                                       recent[B::recent_value(t, dv + 2)] | ((unsigned)recent[B::recent_value(t, dv + 3)] << 16));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = b * kBlock + token + 8 * i;
+                if (t >= first)
+                    kv[i] = *reinterpret_cast<const uint4 *>(k + row(t) * a.k_stride + dk);
+                else if (recent)
+                    kv[i] = *reinterpret_cast<const uint4 *>(recent + B::recent_key(t, dk));
             }
         }
-        unsigned mk = max_bits(kv, 0u), mv = max_bits(make_uint4(vv[0], vv[1], vv[2], vv[3]), 0u);
-        mk = wave_max_bits(mk);
-        mv = wave_max_bits(mv);
-        if ((tid & 63) == 0) {
-            top[0][tid >> 6] = mk;
-            top[1][tid >> 6] = mv;
+        unsigned most = values ? max_bits(make_uint4(vv[2].x, vv[2].y, vv[3].x, vv[3].y), max_bits(make_uint4(vv[0].x, vv[0].y, vv[1].x, vv[1].y), 0u))
+                               : max_bits(kv[1], max_bits(kv[0], 0u));
+        most = wave_max_bits(most);
+        if ((tid & 63) == 0) top[tid >> 6] = most;
+        __syncthreads();
+        unsigned mv = top[0], mk = top[WAVES];
+        if (WAVES == 2) {
+            mv = max(mv, top[1]);
+            mk = max(mk, top[3]);
+        }
+        const uint16_t sv = token_scale(h2f((uint16_t)mv), 127.0f), sk = token_scale(h2f((uint16_t)mk), 127.0f);
+        if (values) {
+            const float s = h2f(sv), inv = 1.0f / s;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint16_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = (uint16_t)((e < 2 ? vv[i].x : vv[i].y) >> 16 * (e & 1));
+                *reinterpret_cast<unsigned *>(block + kBlock * D + value_at(4 * quad, dv + e)) = code4(h, s, inv);
+            }
+        } else {
+            const float s = h2f(sk), inv = 1.0f / s;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint2 q = quant8(kv[i], s, inv, -128.0f, 127.0f);
+                *reinterpret_cast<uint2 *>(block + key_at(token + 8 * i, dk)) = make_uint2(q.x ^ 0x80808080u, q.y ^ 0x80808080u);
+            }
         }
         __syncthreads();
         if (page >= 0) {
-            mk = max(max(top[0][0], top[0][1]), max(top[0][2], top[0][3]));
-            mv = max(max(top[1][0], top[1][1]), max(top[1][2], top[1][3]));
-            const uint16_t sk = token_scale(h2f((uint16_t)mk), 127.0f), sv = token_scale(h2f((uint16_t)mv), 127.0f);
-            uint8_t *codes = B::codes(c, page, head, b);
-            if (KEYS == 256 || tid < KEYS) {
-                uint2 q = quant8(kv, h2f(sk), 1.0f / h2f(sk), -128.0f, 127.0f);
-                *reinterpret_cast<uint2 *>(codes + key_at(token, d)) = make_uint2(q.x ^ 0x80808080u, q.y ^ 0x80808080u);
-            }
-            if (D == 128 || quad < 4) {
-                const float s = h2f(sv), inv = 1.0f / s;
-                uint16_t lo[4], hi[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    lo[i] = (uint16_t)(vv[i] & 0xffffu);
-                    hi[i] = (uint16_t)(vv[i] >> 16);
-                }
-                uint8_t *values = codes + kBlock * D;
-                *reinterpret_cast<unsigned *>(values + value_at(4 * quad, dv)) = code4(lo, s, inv);
-                *reinterpret_cast<unsigned *>(values + value_at(4 * quad, dv + 1)) = code4(hi, s, inv);
-            }
+            reinterpret_cast<uint4 *>(B::codes(c, page, head, b))[tid] = reinterpret_cast<const uint4 *>(block)[tid];
             if (tid == 0) *B::scales(c, page, head, b) = (unsigned)sk | ((unsigned)sv << 16);
         }
     }
     if (!leads || !recent) return;
-    __syncthreads();                                     // the ring has been read
+    __syncthreads();                             // the ring has been read
     const int begin = max(max(first, 0), (full - 1) * kBlock);
-    for (int i = tid; i < (length - begin) * (D / 8); i += 256) {
+    for (int i = tid; i < (length - begin) * (D / 8); i += THREADS) {
         const int t = begin + i / (D / 8), d = i % (D / 8) * 8;
         *reinterpret_cast<uint4 *>(recent + B::recent_key(t, d)) = *reinterpret_cast<const uint4 *>(k + row(t) * a.k_stride + d);
         const uint4 w = *reinterpret_cast<const uint4 *>(v + row(t) * a.v_stride + d);
@@ -285,7 +295,7 @@ flexq_status flexq_cache_append(const flexq_cache *cache, const flexq_sequences 
     if (cache->head_dim == 128)
         hipLaunchKernelGGL(append_kernel<128>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
     else
-        hipLaunchKernelGGL(append_kernel<64>, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+        hipLaunchKernelGGL(append_kernel<64>, dim3((unsigned)grid), dim3(128), 0, (hipStream_t)stream, a);
     return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
 }
 
