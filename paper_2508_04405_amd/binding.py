@@ -668,7 +668,7 @@ def prompt_attention(q, k, v, heads, kv_heads, starts, scale=None, out=None):
     rows starts[i] .. starts[i + 1] - 1 (int32) -> fp16 [M, heads * D].  scale: 1 / sqrt(D) unless given."""
     lib = load()
     cur = _current(q)
-    M, D = q.shape[0], _head_dim(q, heads)
+    D, M = _head_dim(q, heads), q.shape[0]
     count = _sizes(starts, ("sequences + 1",))[0] - 1
     _here(starts, torch.int32, (count + 1,), cur)
     qs, ks, vs = _rows(q, M, heads * D, cur), _rows(k, M, kv_heads * D, cur), _rows(v, M, kv_heads * D, cur)
@@ -722,7 +722,7 @@ def _together(cache, seqs, rows):
 def cache_append(cache, k, v, seqs):
     """fp16 rows k and v [M, kv_heads * D], the newest tokens of the sequences, into the cache."""
     cur, width = _together(cache, seqs, k), cache.kv_heads * cache.head_dim
-    M = k.shape[0]
+    M = _sizes(k, ("rows", "width"))[0]
     _check(load().flexq_cache_append(ctypes.byref(cache.c), ctypes.byref(seqs.c), M, k.data_ptr(), _rows(k, M, width, cur),
                                      v.data_ptr(), _rows(v, M, width, cur), _stream()))
 
@@ -736,7 +736,7 @@ def cache_read(cache, seqs, rows=None, out=None):
             raise FlexQError("flexq: reading takes `out` or a number of rows")
         out = tuple(torch.empty((rows, width), dtype=torch.float16, device=cache.codes.device) for _ in range(2))
     k, v = out
-    cur, M = _together(cache, seqs, k), k.shape[0]
+    cur, M = _together(cache, seqs, k), _sizes(k, ("rows", "width"))[0]
     _check(load().flexq_cache_read(ctypes.byref(cache.c), ctypes.byref(seqs.c), M, k.data_ptr(), _rows(k, M, width, cur),
                                    v.data_ptr(), _rows(v, M, width, cur), _stream()))
     return k, v
@@ -747,7 +747,7 @@ def cache_attention(cache, q, heads, seqs, scale=None, workspace=None, out=None)
     [M, heads * D]: row i of n of a sequence of length L sees tokens 0 .. L - n + i.  scale: 1 / sqrt(D) unless given."""
     lib = load()
     cur, D = _together(cache, seqs, q), cache.head_dim
-    M = q.shape[0]
+    M = _sizes(q, ("rows", "width"))[0]
     stride = _rows(q, M, heads * D, cur)
     ws = _scratch(lib.flexq_cache_attention_workspace_bytes(M, seqs.count, heads, cache.kv_heads, D), workspace, q.device, cur)
     if out is None:

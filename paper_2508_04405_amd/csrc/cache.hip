@@ -143,11 +143,10 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs a)
     }
 }
 
-// fp16 of a code times its scale, the largest finite one where that is beyond them.
+// fp16 of a code times its scale.
 __device__ __forceinline__ unsigned value2(unsigned lo, unsigned hi, float s)
 {
-    return pack_h2(__builtin_amdgcn_fmed3f((float)((int)lo - kCodeBias) * s, -65504.0f, 65504.0f),
-                   __builtin_amdgcn_fmed3f((float)((int)hi - kCodeBias) * s, -65504.0f, 65504.0f));
+    return pack_h2(within_half((float)((int)lo - kCodeBias) * s), within_half((float)((int)hi - kCodeBias) * s));
 }
 
 template <int D>

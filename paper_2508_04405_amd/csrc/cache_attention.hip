@@ -212,15 +212,15 @@ __device__ __forceinline__ void take(Running<D, RB> &r, const float (&x)[RB][2][
     }
 }
 
-// Four channels of row `row` of a sequence's and key head's rows: o / l, 65504 at most (a scale's own rounding may lead
-// beyond); zero where the row sees nothing.
+// Four channels of row `row` of a sequence's and key head's rows: o / l; zero where
+// the row sees nothing.
 __device__ __forceinline__ void store_row(const CachedArgs &a, int begin, int row, int head, int D, int d, v4f o, float l)
 {
     const int token = row / a.group;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     v4f y = o * inv;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(y[i], -65504.0f, 65504.0f);
+    for (int i = 0; i < 4; ++i) y[i] = within_half(y[i]);
     uint16_t *out = a.out + (size_t)(begin + token) * a.out_stride + (size_t)(head * a.group + row - token * a.group) * D + d;
     *reinterpret_cast<uint2 *>(out) = make_uint2(pack_h2(y[0], y[1]), pack_h2(y[2], y[3]));
 }
@@ -619,7 +619,8 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                 float scale[kStageBlocks], lv[kStageBlocks], back[kStageBlocks];
                 {
                     const bool code = sc != 0u, ring = has_tail && recent && kStageBlocks * s + mine == full;
-                    const float k = code ? h2f((uint16_t)(sc & 0xffffu)) * a.scale : a.scale;
+                    // (a scale is not zero, also where the product is below the smallest number: hidden scores are -inf times it)
+                    const float k = code ? fmaxf(h2f((uint16_t)(sc & 0xffffu)) * a.scale, 1e-38f) : a.scale;
                     const float v = code ? __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16))) : ring ? 0.0f : -INFINITY;
                     const float inv = code || ring ? __builtin_amdgcn_exp2f(-v) : 0.0f;
 #pragma unroll

@@ -250,7 +250,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             *reinterpret_cast<uint2 *>(out + 32 * t + 8 * i) = make_uint2(
-                pack_h2(o[t][4 * i] * inv, o[t][4 * i + 1] * inv), pack_h2(o[t][4 * i + 2] * inv, o[t][4 * i + 3] * inv));
+                pack_h2(within_half(o[t][4 * i] * inv), within_half(o[t][4 * i + 1] * inv)),
+                pack_h2(within_half(o[t][4 * i + 2] * inv), within_half(o[t][4 * i + 3] * inv)));
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

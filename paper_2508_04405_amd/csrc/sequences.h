@@ -34,6 +34,12 @@ typedef float v2f __attribute__((ext_vector_type(2)));
 constexpr int kBlock = FLEXQ_CACHE_BLOCK;    // tokens that share a scale
 constexpr int kCodeBias = 128;               // codes are stored as code + 128
 
+// The largest finite fp16 at most: the rounding of weights, or of a scale, may lead a mean of finite values beyond it.
+__device__ __forceinline__ float within_half(float y)
+{
+    return __builtin_amdgcn_fmed3f(y, -65504.0f, 65504.0f);
+}
+
 struct RowRange {
     int id, begin, n;    // sequence (-1: none), its first row, its rows
     int piece;           // number of the piece within the sequence

@@ -124,6 +124,42 @@ def test_prompt_flat_and_peaked(size, scale):
     check_prompt(q, k, v, [n], heads, kv, got, scale)
 
 
+def test_prompt_of_many_rows():
+    """As many rows as take 256 to a workgroup; some of every sequence against the plain form."""
+    rng = np.random.default_rng(10)
+    heads, kv, D, parts = 64, 8, 128, [1500, 1, 2600, 7, 120, 31]
+    M = sum(parts)
+    q, k, v = normal(rng, M, heads * D), keys(rng, M, kv * D), normal(rng, M, kv * D)
+    got = host(fq.prompt_attention(to_dev(q), to_dev(k), to_dev(v), heads, kv, starts_of(parts)))
+    assert np.isfinite(got).all()
+    at = 0
+    for n in parts:
+        for lo in sorted({0, n // 3, n // 2, max(n - 5, 0)}):
+            hi = min(lo + 5, n)
+            want, off = ref.grouped(q[at + lo:at + hi], k[at:at + hi], v[at:at + hi], heads, kv, lo, D ** -0.5)
+            assert_within(got[at + lo:at + hi], want, off, f"rows {lo} .. {hi} of {n}")
+        at += n
+
+
+def test_prompt_of_the_smallest_scale():
+    rng = np.random.default_rng(24)
+    q, k, v = normal(rng, 70, 128), normal(rng, 70, 64), normal(rng, 70, 64)
+    got = host(fq.prompt_attention(to_dev(q), to_dev(k), to_dev(v), 2, 1, starts_of([70]), scale=1.4e-45))
+    check_prompt(q, k, v, [70], 2, 1, got, 1.4e-45)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_prompt_of_the_largest_values(sign):
+    """Weights whose rounding goes up: 512 and, from the second key on, 256.13, which fp16 takes for 256.25.  The mean of
+    equal values is not beyond them."""
+    n, D = 200, 64
+    q, k, v = np.zeros((n, D), np.float16), np.zeros((n, D), np.float16), np.full((n, D), sign * 65504.0, np.float16)
+    q[:, 0] = 1
+    k[0, 0] = 1
+    got = host(fq.prompt_attention(to_dev(q), to_dev(k), to_dev(v), 1, 1, starts_of([n]), scale=0.69265))
+    check_prompt(q, k, v, [n], 1, 1, got, 0.69265)
+
+
 def test_prompt_many_sequences():
     rng = np.random.default_rng(11)
     parts = rng.integers(0, 9, 700).tolist()
@@ -279,6 +315,90 @@ def test_cached_attention_of_many_sequences():
     s.check_attention(rng.integers(0, lengths + 1).tolist(), 8)
 
 
+@pytest.mark.parametrize("heads,kv,D", [(8, 1, 64), (16, 2, 128)])
+def test_chunks_of_many_sequences(heads, kv, D):
+    """More than 64 rows of a sequence on average, of more than 64 sequences, some without rows, some without tokens."""
+    rng = np.random.default_rng([19, D])
+    count = 70
+    new = rng.integers(0, 40, count)
+    new[:4] = 0, 200, 1, 0
+    before = rng.integers(0, 150, count)
+    before[3] = 0
+    s = Story(rng, count, kv, D, 32, 352)
+    s.append(before.tolist())
+    s.append(new.tolist())
+    assert new.sum() * (heads // kv) / count > 64
+    s.check_attention(new.tolist(), heads)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_that_see_nothing_or_not_all(D):
+    rng = np.random.default_rng([20, D])
+    kv, heads = 1, 8
+    s = Story(rng, 3, kv, D, 16, 128)
+    s.append([60, 80, 90])
+    s.append([40, 30, 10])
+    parts = (40, 30, 10)
+    q = normal(rng, 80, heads * D)
+    k, v = [ref.stored(x, kv) for x in s.k], [ref.stored(x, kv) for x in s.v]
+
+    def run(lengths=(100, 110, 100), table=s.table, slots=s.slots, scale=None):
+        seqs = fq.Sequences(starts_of(parts), i32(list(lengths)), to_dev(np.ascontiguousarray(table)), to_dev(slots))
+        return host(fq.cache_attention(s.cache, to_dev(q), heads, seqs, scale=scale))
+
+    def check(out, rows, k, v, first, scale=D ** -0.5):
+        want, off = ref.grouped(q[rows], k, v, heads, kv, first, scale)
+        assert_within(out[rows], want, off)
+
+    # lengths below the rows: the first ones see nothing
+    out = run(lengths=(16, 0, -3))
+    assert not out[:24].any() and not out[40:].any()
+    check(out, slice(24, 40), k[0][:16], v[0][:16], 0)
+    # pages that are not there, the last one, which the unfinished block would go to, among them
+    table = s.table.copy()
+    table[0, 1], table[0, 6], table[1, :] = -1, 2**30, 2**31 - 1
+    out = run(table=table)
+    left = np.r_[0:16, 32:100]
+    check(out, slice(0, 40), k[0][left], v[0][left], 44)
+    # (the second sequence's pages: none; its unfinished block begins at 96, and its rows at 80)
+    assert not out[40:56].any()
+    check(out, slice(56, 70), k[1][96:], v[1][96:], 0)
+    # slots that are not there
+    out = run(slots=np.array([-1, 3, -2**31], np.int32))
+    for rows, i, first in ((slice(0, 40), 0, 60), (slice(40, 70), 1, 80), (slice(70, 80), 2, 90)):
+        check(out, rows, k[i][:96], v[i][:96], first)
+    # the smallest scale, which a small scale of keys would take to zero
+    out = run(scale=1.4e-45)
+    for rows, i, first in ((slice(0, 40), 0, 60), (slice(40, 70), 1, 80), (slice(70, 80), 2, 90)):
+        check(out, rows, k[i], v[i], first, 1.4e-45)
+
+
+def test_a_length_beyond_the_table_counts_as_its_end():
+    rng = np.random.default_rng(21)
+    s = Story(rng, 2, 1, 64, 16, 64)
+    s.append([64, 20])
+    q = to_dev(normal(rng, 4, 4 * 64))
+    call = lambda first: host(fq.cache_attention(s.cache, q, 4, fq.Sequences(i32([0, 2, 4]), i32([first, 20]), to_dev(s.table),
+                                                                           to_dev(s.slots))))
+    want = call(64)
+    for length in (65, 1000, 2**31 - 1):
+        assert np.array_equal(call(length), want)
+
+
+@pytest.mark.parametrize("n", [1, 12, 40])
+def test_sequences_that_share_pages(n):
+    """A beginning that two sequences have in common, in the same pages; tokens of their own behind it."""
+    rng = np.random.default_rng([22, n])
+    kv, D, heads, page = 2, 128, 4, 32
+    s = Story(rng, 2, kv, D, page, 256)
+    s.append([128, 0])
+    s.table[1, :4] = s.table[0, :4]
+    s.k[1], s.v[1] = s.k[0].copy(), s.v[0].copy()
+    s.append([n, n])
+    s.check_read(s.lengths())
+    s.check_attention([n, n], heads)
+
+
 def test_values_of_very_different_sizes():
     """Blocks whose values' scales are 2^20 apart."""
     rng = np.random.default_rng(13)
@@ -374,6 +494,42 @@ def test_a_captured_step_follows_lengths_and_pages():
             want, off = ref.grouped(qh[i:i + 1], ref.stored(s.k[i], kv), ref.stored(s.v[i], kv), heads, kv, len(s.k[i]) - 1, D ** -0.5)
             assert_within(got[i:i + 1], want, off, f"step {step} sequence {i}")
     del kk, vv
+
+
+def test_two_graphs_share_a_workspace():
+    """Chunks of two sequences' prompts and single tokens, in graphs of one workspace, replayed in turn with eager calls and a
+    changed batch between them."""
+    rng = np.random.default_rng(23)
+    kv, D, heads = 1, 64, 8
+    s = Story(rng, 2, kv, D, 32, 700)
+    s.append([600, 333])
+    shapes = [[30, 25], [1, 1]]
+    seqs = [s.seqs(parts) for parts in shapes]
+    q = [torch.zeros((sum(parts), heads * D), dtype=torch.float16, device=DEV) for parts in shapes]
+    k = [torch.zeros((sum(parts), kv * D), dtype=torch.float16, device=DEV) for parts in shapes]
+    out = [torch.empty_like(x) for x in q]
+    own = [torch.empty_like(x) for x in q]
+    need = max(fq.load().flexq_cache_attention_workspace_bytes(sum(p), 2, heads, kv, D) for p in shapes)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in shapes]
+    for i, graph in enumerate(graphs):
+        with torch.cuda.graph(graph):
+            fq.cache_attention(s.cache, q[i], heads, seqs[i], workspace=ws, out=out[i])
+            fq.prompt_attention(q[i], k[i], k[i], heads, kv, seqs[i].starts, out=own[i])
+    for step in range(5):
+        for i, graph in enumerate(graphs):
+            q[i].copy_(to_dev(normal(rng, *q[i].shape)))
+            k[i].copy_(to_dev(normal(rng, *k[i].shape)))
+            seqs[i].lengths.copy_(i32([600 - 37 * step, 333 - 16 * step]))
+            out[i].fill_(NAN)
+            own[i].fill_(NAN)
+            graph.replay()
+            got, got_own = host(out[i]), host(own[i])
+            ws.fill_(255)
+            assert np.array_equal(got, host(fq.cache_attention(s.cache, q[i], heads, seqs[i])))
+            assert np.array_equal(got_own, host(fq.prompt_attention(q[i], k[i], k[i], heads, kv, seqs[i].starts)))
+            assert np.isfinite(got).all() and np.isfinite(got_own).all()
 
 
 def test_two_streams_at_once():
