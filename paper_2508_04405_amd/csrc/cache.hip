@@ -52,8 +52,8 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs a)
     __shared__ unsigned top[2 * WAVES];
     __shared__ __attribute__((aligned(16))) uint8_t block[B::kBytes];    // the block's codes as they go out, 16 bytes a thread
     const CacheArgs &c = a.c;
-    const int tid = threadIdx.x, head = blockIdx.x % c.kv_heads;
-    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, blockIdx.x / c.kv_heads);
+    const int tid = threadIdx.x, index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
+    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, index);
     if (r.id < 0 || r.n == 0) return;
     const int length = cached_length(c, r.id), first = length - r.n;         // (may be negative: those rows are dropped)
     const int b0 = max(first, 0) / kBlock, b = b0 + r.piece, full = length / kBlock;
@@ -155,8 +155,8 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
     typedef CacheBlock<D> B;
     constexpr int KEYS = kBlock * D / 8;
     const CacheArgs &c = a.c;
-    const int tid = threadIdx.x, head = blockIdx.x % c.kv_heads;
-    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, blockIdx.x / c.kv_heads);
+    const int tid = threadIdx.x, index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
+    const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, index);
     if (r.id < 0 || r.n == 0) return;
     const int length = cached_length(c, r.id), first = length - r.n;
     // (first may be negative: the block of a negative token has none, its rows are zero)
@@ -235,6 +235,7 @@ flexq_status cache_args(const flexq_cache *C, const flexq_sequences *S, int M, C
     c.slots = S->slots;
     c.page_bytes = page_bytes;
     c.kv_heads = C->kv_heads;
+    c.by_kv = divider(C->kv_heads);
     c.pages = C->pages;
     c.slot_count = C->slots;
     c.shift = __builtin_ctz((unsigned)C->page / kBlock);

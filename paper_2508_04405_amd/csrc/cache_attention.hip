@@ -37,6 +37,7 @@ struct CachedArgs {
     float *part;                                 // [kv_heads][parts][2][rows of a tile][D + 4]: output, running maximum, sum
     float scale;                                 // times log2 e
     int group, heads, parts;                     // heads of a key head; workgroups of a key head
+    Divider by_group, by_parts;
     int least;                                   // steps that a workgroup takes at least
 };
 
@@ -104,7 +105,7 @@ struct Steps {
 // Part i of the steps is i * width .. (i + 1) * width - 1.
 __device__ __forceinline__ int part_width(const CachedArgs &a, int total)
 {
-    return max((total + a.parts - 1) / a.parts, a.least);
+    return max(divide(total + a.parts - 1, a.by_parts), a.least);
 }
 
 __device__ __forceinline__ v4f mfma_h(v8h a, v8h b, v4f c)
@@ -216,7 +217,7 @@ __device__ __forceinline__ void take(Running<D, RB> &r, const float (&x)[RB][2][
 // the row sees nothing.
 __device__ __forceinline__ void store_row(const CachedArgs &a, int begin, int row, int head, int D, int d, v4f o, float l)
 {
-    const int token = row / a.group;
+    const int token = divide(row, a.by_group);
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     v4f y = o * inv;
 #pragma unroll
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     __shared__ float stat[kWaves][2][16];
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i16 = lane & 15;
-    const int head = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
+    const int index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
     Steps<ROWS, 2 * kBlock> all(a);
     const int total = all.all(), width = part_width(a, total);
     int at = index * width;
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         v8h q[RB][D / 32];
 #pragma unroll
         for (int k = 0; k < RB; ++k) {
-            const int row = p.tile * ROWS + min(16 * k + i16, rows - 1), token = row / a.group;
+            const int row = p.tile * ROWS + min(16 * k + i16, rows - 1), token = divide(row, a.by_group);
             limit[k] = p.length - p.n + token;
             const uint16_t *from = a.q + (size_t)(p.begin + token) * a.q_stride + (size_t)(head * a.group + row - token * a.group) * D;
 #pragma unroll
@@ -273,8 +274,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
             for (int t = 0; t < D / 16; ++t) r.o[k][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         }
         const int full = p.length / kBlock;                                  // blocks in pages
-        const int sees_first = p.length - p.n + p.tile * ROWS / a.group;     // last key that the first row sees
-        const int seen = p.length - p.n + (p.tile * ROWS + rows - 1) / a.group + 1;      // keys that any of the rows sees
+        const int sees_first = p.length - p.n + divide(p.tile * ROWS, a.by_group);     // last key that the first row sees
+        const int seen = p.length - p.n + divide(p.tile * ROWS + rows - 1, a.by_group) + 1;      // keys that any of the rows sees
         const int blocks = min(full, (max(seen, 0) + kBlock - 1) / kBlock);
         const int done = min(last, (blocks + 1) / 2);                        // steps over pages end here
         // pages a step ahead of the loads, loads a step ahead of the products; steps past the end repeat the last block
@@ -440,7 +441,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // prompts' kernel read them, so that a code is turned once for 128 rows.  A block of 16 keys is half of a result's
 // registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is raised only where a lane's weights of
 // a block add up to more than 2^15.
-constexpr int kStageKeys = 64, kStageBlocks = 4, kStageWaves = 4, kStageRows = 32 * kStageWaves;
+constexpr int kStageWaves = 4, kStageRows = 32 * kStageWaves;
+constexpr int stage_keys(int D) { return D == 64 ? 128 : 64; }
 constexpr float kStageShift = 9.0f, kMost = 32768.0f;
 
 __device__ __forceinline__ v16f mfma_h(v8h a, v8h b, v16f c)
@@ -452,19 +454,22 @@ template <int D>
 __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_eu(2))) void chunk_kernel(CachedArgs a)
 {
     typedef CacheBlock<D> B;
+    constexpr int KEYS = stage_keys(D), BLOCKS = KEYS / kBlock;
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
     // keys: a line of D channels each; values: a line of 64 keys for each channel, chunk 2 b + half of 16 bytes holding keys
     // 16 b + 4 half + {0 .. 3, 8 .. 11}; chunks XORed by the line, so that sixteen lines' same chunk meets every bank once
-    constexpr int LINE = 2 * D, KSTAGE = kStageKeys * LINE, VSTAGE = D * 2 * kStageKeys;
-    constexpr int TASKS = kStageBlocks * D / 64 / kStageWaves;           // planes of 1 KiB of a wavefront, of keys and of values
+    constexpr int LINE = 2 * D, VLINE = 2 * KEYS, KSTAGE = KEYS * LINE, VSTAGE = D * VLINE;
+    constexpr int TASKS = BLOCKS * D / 64 / kStageWaves;           // planes of 1 KiB of a wavefront, of keys and of values
     static_assert(TASKS >= 1, "every wavefront has a plane");
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][KSTAGE + VSTAGE];
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
-    const int head = blockIdx.x % c.kv_heads, index = blockIdx.x / c.kv_heads;
+    // workgroups 8 apart share an XCD and its L2: each XCD has neighbouring parts, which read the same keys at about the same time
+    const int xcd = blockIdx.x % 8, per = gridDim.x / 8, more = gridDim.x % 8;
+    const int id = xcd * per + min(xcd, more) + (int)blockIdx.x / 8, head = divide(id, a.by_parts), index = id - head * a.parts;
     auto key_swizzle = [](int line) { return D == 128 ? line & 15 : (line >> 1) & 7; };
-    auto value_swizzle = [](int line) { return (line >> 1) & 7; };
-    Steps<kStageRows, kStageKeys> all(a);
+    auto value_swizzle = [](int line) { return KEYS == 128 ? line & 15 : (line >> 1) & 7; };
+    Steps<kStageRows, KEYS> all(a);
     const int total = all.all(), width = part_width(a, total);
     int at = index * width;
     const int stop = min(at + width, total);
@@ -475,15 +480,16 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
         const int first = at - p.first, last = end - p.first;            // stages of the tile
         const bool whole = first == 0 && last == p.steps;
         const int row0 = p.tile * kStageRows, rows = min(kStageRows, p.n * a.group - row0);
-        const int row = row0 + min(32 * wave + i32, rows - 1), token = row / a.group, limit = p.length - p.n + token;
+        const int row = row0 + min(32 * wave + i32, rows - 1), token = divide(row, a.by_group), limit = p.length - p.n + token;
         const bool some = 32 * wave < rows;
         const int w_last = row0 + min(32 * wave + 31, rows - 1);
-        const int sees_first = p.length - p.n + (row0 + 32 * wave) / a.group, sees_last = some ? p.length - p.n + w_last / a.group : -1;
-        const int seen = p.length - p.n + (row0 + rows - 1) / a.group + 1;       // keys that any of the rows sees
+        const int sees_first = p.length - p.n + divide(row0 + 32 * wave, a.by_group);
+        const int sees_last = some ? p.length - p.n + divide(w_last, a.by_group) : -1;
+        const int seen = p.length - p.n + divide(row0 + rows - 1, a.by_group) + 1;       // keys that any of the rows sees
         const int full = p.length / kBlock, tail = p.length - full * kBlock;
         const int blocks = min(full, (max(seen, 0) + kBlock - 1) / kBlock);      // in pages
         const bool has_tail = tail > 0 && seen > full * kBlock;
-        const int done = min(last, (blocks + (has_tail ? 1 : 0) + kStageBlocks - 1) / kStageBlocks);
+        const int done = min(last, (blocks + (has_tail ? 1 : 0) + BLOCKS - 1) / BLOCKS);
         const uint16_t *recent = B::recent(c, p.id, head);
         v8h q[D / 16];
         {
@@ -496,24 +502,24 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
         int pages = -1;
         unsigned scales = 0u;
         bool there = false;
-        const int mine = lane & (kStageBlocks - 1);
+        const int mine = lane & (BLOCKS - 1);
         // planes of a stage: number n of a wavefront is plane n + TASKS wave, plane j of block b being D / 64 b + j
         auto block_of = [&](int n) { return (TASKS * wave + n) / (D / 64); };
         auto ask_pages = [&](int s) {
-            pages = c.table[(size_t)p.id * c.max_pages + (max(min(kStageBlocks * s + mine, blocks - 1), 0) >> c.shift)];
+            pages = c.table[(size_t)p.id * c.max_pages + (max(min(BLOCKS * s + mine, blocks - 1), 0) >> c.shift)];
         };
         auto fetch = [&](int s) {                    // (after ask_pages of the same stage)
             const bool valid = pages >= 0 && pages < c.pages;
             const int good = valid ? pages : 0;
-            there = valid && kStageBlocks * s + mine < blocks;
+            there = valid && BLOCKS * s + mine < blocks;
 #pragma unroll
             for (int n = 0; n < TASKS; ++n) {
-                const int block = min(kStageBlocks * s + block_of(n), max(blocks - 1, 0)), plane = (TASKS * wave + n) % (D / 64);
+                const int block = min(BLOCKS * s + block_of(n), max(blocks - 1, 0)), plane = (TASKS * wave + n) % (D / 64);
                 const uint8_t *codes = B::codes(c, __builtin_amdgcn_readlane(good, block_of(n)), head, block);
                 k_codes[n] = reinterpret_cast<const v4u *>(codes + 1024 * plane)[lane];
                 v_codes[n] = reinterpret_cast<const v4u *>(codes + kBlock * D + 1024 * plane)[lane];
             }
-            scales = *B::scales(c, good, head, there ? kStageBlocks * s + mine : 0);
+            scales = *B::scales(c, good, head, there ? BLOCKS * s + mine : 0);
         };
         auto put = [&](int s) {
             uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
@@ -535,7 +541,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int channel = 64 * plane + 16 * (t + h) + i;
-                        *reinterpret_cast<v2u *>(vs + channel * 128 + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) = w.u[h];
+                        *reinterpret_cast<v2u *>(vs + channel * VLINE + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) = w.u[h];
                     }
                 }
             }
@@ -543,7 +549,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
         // the unfinished block's tokens over what was put in its place
         auto put_tail = [&](int s) {
             uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
-            const int b = full - kStageBlocks * s;
+            const int b = full - BLOCKS * s;
             for (int u = threadIdx.x; u < kBlock * (D / 8); u += 64 * kStageWaves) {
                 const int t = u / (D / 8), chunk = u % (D / 8), line = kBlock * b + t;
                 v4u w = {0u, 0u, 0u, 0u};
@@ -559,7 +565,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                     for (int e = 0; e < 4; ++e)
                         if (4 * g + e < tail) w[e] = from[e];
                 }
-                *reinterpret_cast<v2u *>(vs + channel * 128 + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) =
+                *reinterpret_cast<v2u *>(vs + channel * VLINE + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) =
                     v2u{(unsigned)w[0] | ((unsigned)w[1] << 16), (unsigned)w[2] | ((unsigned)w[3] << 16)};
             }
         };
@@ -571,7 +577,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
         auto prepare = [&](int s) {                  // stage s, asked for, into its buffer
             put(s);
-            if (has_tail && full / kStageBlocks == s) {
+            if (has_tail && full / BLOCKS == s) {
                 __syncthreads();
                 put_tail(s);
             }
@@ -592,56 +598,58 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                 fetch(s + 1);
                 ask_pages(s + 2);
             }
-            if (some && kStageKeys * s <= sees_last) {
+            if (some && KEYS * s <= sees_last) {
                 const uint8_t *ks = lds[s & 1], *vs = ks + KSTAGE;
-                v16f x[2];
+                v16f x[BLOCKS / 2];
                 {
                     constexpr int AHEAD = 4;         // operands asked for ahead of the instruction that takes them
                     v8h ring[AHEAD];
-                    auto key_part = [&](int n) {     // n: keys 32 (n % 2) .., channels 16 (n / 2) ..
-                        const int line = 32 * (n & 1) + i32;
-                        return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * (((n & ~1) + half) ^ key_swizzle(line)));
+                    constexpr int U = BLOCKS / 2;
+                    auto key_part = [&](int n) {     // n: keys 32 (n % U) .., channels 16 (n / U) ..
+                        const int line = 32 * (n % U) + i32;
+                        return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * ((2 * (n / U) + half) ^ key_swizzle(line)));
                     };
 #pragma unroll
                     for (int n = 0; n < AHEAD; ++n) ring[n] = key_part(n);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < BLOCKS / 2; ++u)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) x[u][i] = 0.0f;
 #pragma unroll
-                    for (int n = 0; n < D / 8; ++n) {
-                        x[n & 1] = mfma_h(ring[n % AHEAD], q[n >> 1], x[n & 1]);
-                        if (n + AHEAD < D / 8) ring[n % AHEAD] = key_part(n + AHEAD);
+                    for (int n = 0; n < D / 16 * U; ++n) {
+                        x[n % U] = mfma_h(ring[n % AHEAD], q[n / U], x[n % U]);
+                        if (n + AHEAD < D / 16 * U) ring[n % AHEAD] = key_part(n + AHEAD);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
                 // the blocks' scales: of keys, with the call's; of values, their logarithm and what takes it back
-                float scale[kStageBlocks], lv[kStageBlocks], back[kStageBlocks];
+                float scale[BLOCKS], lv[BLOCKS], back[BLOCKS];
                 {
-                    const bool code = sc != 0u, ring = has_tail && recent && kStageBlocks * s + mine == full;
+                    const bool code = sc != 0u, ring = has_tail && recent && BLOCKS * s + mine == full;
                     // (a scale is not zero, also where the product is below the smallest number: hidden scores are -inf times it)
                     const float k = code ? fmaxf(h2f((uint16_t)(sc & 0xffffu)) * a.scale, 1e-38f) : a.scale;
                     const float v = code ? __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16))) : ring ? 0.0f : -INFINITY;
                     const float inv = code || ring ? __builtin_amdgcn_exp2f(-v) : 0.0f;
 #pragma unroll
-                    for (int b = 0; b < kStageBlocks; ++b) {
+                    for (int b = 0; b < BLOCKS; ++b) {
                         scale[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k), b));
                         lv[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), b));
                         back[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(inv), b));
                     }
                 }
-                if (kStageKeys * (s + 1) - 1 > sees_first) {
+                if (KEYS * (s + 1) - 1 > sees_first) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < BLOCKS / 2; ++u)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (kStageKeys * s + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3) > limit) x[u][i] = -INFINITY;
+                            if (KEYS * s + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3) > limit) x[u][i] = -INFINITY;
                 }
-                v8h w[2][2];
-                float part[kStageBlocks];
+                v8h w[BLOCKS / 2][2];
+                float part[BLOCKS];
+                __builtin_amdgcn_s_setprio(0);
                 auto weights = [&] {
 #pragma unroll
-                    for (int b = 0; b < kStageBlocks; ++b) {
+                    for (int b = 0; b < BLOCKS; ++b) {
                         const float less = top - kStageShift - lv[b];
                         part[b] = 0.0f;
 #pragma unroll
@@ -654,13 +662,21 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                             w[b / 2][b & 1][i] = h[0];
                             w[b / 2][b & 1][i + 1] = h[1];
                         }
+                        asm volatile("" : "+v"(w[b / 2][b & 1]));    // (in fp16 from here on, not once all are weighed)
                     }
                 };
-                weights();
-                if (__any(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) > kMost)) {
+                bool above = s == first;             // (at the first stage every score is far above m)
+                if (!above) {
+                    weights();
+                    float most = part[0];
+#pragma unroll
+                    for (int b = 1; b < BLOCKS; ++b) most = fmaxf(most, part[b]);
+                    above = __any(most > kMost);
+                }
+                if (above) {
                     float best = kNothing;
 #pragma unroll
-                    for (int b = 0; b < kStageBlocks; ++b)
+                    for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) best = fmaxf(best, x[b / 2][8 * (b & 1) + i] * scale[b] + lv[b]);
                     auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
@@ -674,15 +690,25 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                         for (int i = 0; i < 16; ++i) o[t][i] *= f;
                     weights();
                 }
-                sum += (part[0] * back[0] + part[1] * back[1]) + (part[2] * back[2] + part[3] * back[3]);
 #pragma unroll
-                for (int b = 0; b < kStageBlocks; ++b)
+                for (int b = 0; b < BLOCKS; b += 2) sum += part[b] * back[b] + part[b + 1] * back[b + 1];
+                {
+                    __builtin_amdgcn_s_setprio(1);           // (matrix instructions first)
+                    constexpr int T = D / 32, AHEAD = 4;
+                    v8h ring[AHEAD];
+                    auto value_part = [&](int n) {   // n: keys 16 (n / T) .., channels 32 (n % T) ..
+                        const int channel = 32 * (n % T) + i32;
+                        return *reinterpret_cast<const v8h *>(vs + channel * VLINE + 16 * ((2 * (n / T) + half) ^ value_swizzle(channel)));
+                    };
 #pragma unroll
-                    for (int t = 0; t < D / 32; ++t) {
-                        const int channel = 32 * t + i32;
-                        o[t] = mfma_h(*reinterpret_cast<const v8h *>(vs + channel * 128 + 16 * ((2 * b + half) ^ value_swizzle(channel))),
-                                      w[b / 2][b & 1], o[t]);
+                    for (int n = 0; n < AHEAD; ++n) ring[n] = value_part(n);
+#pragma unroll
+                    for (int n = 0; n < BLOCKS * T; ++n) {
+                        o[n % T] = mfma_h(ring[n % AHEAD], w[n / T / 2][n / T & 1], o[n % T]);
+                        if (n + AHEAD < BLOCKS * T) ring[n % AHEAD] = value_part(n + AHEAD);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                }
             }
             if (s + 1 < done) prepare(s + 1);
         }
@@ -716,13 +742,14 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
 // the tile that begins in part i and does not end there, if there is one: with many rows 256 / D of them, a row of few shares
 // each; with few rows one, whose shares its lanes take in turn.
 template <int D, int ROWS, int KEYS>
-__global__ __launch_bounds__(64) void join_kernel(CachedArgs a, int groups)
+__global__ __launch_bounds__(64) void join_kernel(CachedArgs a, Divider by_groups)
 {
     constexpr int Q = D / 4, SHARES = ROWS == kStageRows ? 1 : 64 / Q, HIGH = 64 / Q / SHARES, U = 8;    // Q: lanes of a row
     __shared__ __attribute__((aligned(16))) float red[SHARES][D];
     __shared__ float stat[SHARES][2];
     const CacheArgs &c = a.c;
-    const int head = blockIdx.x % c.kv_heads, group = blockIdx.x / c.kv_heads % groups, index = blockIdx.x / c.kv_heads / groups;
+    const int all_groups = divide(blockIdx.x, c.by_kv), head = blockIdx.x - all_groups * c.kv_heads;
+    const int index = divide(all_groups, by_groups), group = all_groups - index * (int)by_groups.d;
     Steps<ROWS, KEYS> all(a);
     const int total = all.all(), width = part_width(a, total);
     const int start = index * width, stop = start + width;
@@ -834,21 +861,23 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     a.heads = heads;
     const int rows = tile_rows(M, seqs->count, a.group), most = (long)M * a.group < rows ? M * a.group : rows;
     a.parts = parts_for(kv, rows);
-    a.least = rows == kStageRows ? 4 : 8;
+    a.by_group = divider(a.group);
+    a.by_parts = divider(a.parts);
+    a.least = rows == kStageRows ? 256 / stage_keys(D) : 8;
     const int groups = rows == kStageRows ? (most + 256 / D - 1) / (256 / D) : most;     // of rows of a tile
     if ((long)a.parts * kv * groups >= (1L << 26)) return FLEXQ_ESHAPE;  // 64 threads each, 2^32 a launch
     hipStream_t st = (hipStream_t)stream;
     auto run = [&](auto kern, int waves, auto join) {
         hipLaunchKernelGGL(kern, dim3((unsigned)(a.parts * kv)), dim3(64 * waves), 0, st, a);
         if (hipGetLastError() != hipSuccess) return FLEXQ_EHIP;
-        if (a.parts > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.parts * kv * groups)), dim3(64), 0, st, a, groups);
+        if (a.parts > 1) hipLaunchKernelGGL(join, dim3((unsigned)(a.parts * kv * groups)), dim3(64), 0, st, a, divider(groups));
         return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
     };
     if (D == 128)
-        return rows == kStageRows ? run(chunk_kernel<128>, kStageWaves, join_kernel<128, kStageRows, kStageKeys>)
+        return rows == kStageRows ? run(chunk_kernel<128>, kStageWaves, join_kernel<128, kStageRows, stage_keys(128)>)
                : rows == 32       ? run(cached_kernel<128, 2>, kWaves, join_kernel<128, 32, 2 * kBlock>)
                                   : run(cached_kernel<128, 1>, kWaves, join_kernel<128, 16, 2 * kBlock>);
-    return rows == kStageRows ? run(chunk_kernel<64>, kStageWaves, join_kernel<64, kStageRows, kStageKeys>)
+    return rows == kStageRows ? run(chunk_kernel<64>, kStageWaves, join_kernel<64, kStageRows, stage_keys(64)>)
            : rows == 32       ? run(cached_kernel<64, 2>, kWaves, join_kernel<64, 32, 2 * kBlock>)
                               : run(cached_kernel<64, 1>, kWaves, join_kernel<64, 16, 2 * kBlock>);
 }

@@ -38,7 +38,8 @@ struct PromptArgs {
     uint16_t *out;
     const int32_t *starts;
     size_t q_stride, k_stride, v_stride, out_stride;
-    int M, count, group, kv_heads;
+    int M, count, group, kv_heads, pieces;       // pieces: workgroups of a key head
+    Divider by_group, by_kv;
     float scale;                                 // times log2 e
 };
 
@@ -73,29 +74,31 @@ __device__ __forceinline__ int value_swizzle(int line)
     return D == 128 ? 4 * (line & 3) : 4 * ((line >> 1) & 1);
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, int SPLIT>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void prompt_kernel(PromptArgs a)
 {
-    constexpr int ROWS = 32 * WAVES, LINE = 2 * D, CH = D / 8;           // LINE: bytes of a staged row; CH: its chunks
+    // SPLIT wavefronts share 32 rows, each with its keys of every stage
+    constexpr int ROWS = 32 * WAVES / SPLIT, NB = kKeys / 32 / SPLIT;     // NB: blocks of 32 keys of a wavefront
+    constexpr int LINE = 2 * D, CH = D / 8;           // LINE: bytes of a staged row; CH: its chunks
     constexpr int STAGE = kKeys * LINE, DMA = STAGE / 1024 / WAVES;      // DMA: loads of a wavefront for keys, or values
     static_assert(STAGE % (1024 * WAVES) == 0, "a stage is whole loads of every wavefront");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][STAGE];  // [buffer][keys, values]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
-    const int head = blockIdx.x % a.kv_heads;
-    const int pieces = gridDim.x / a.kv_heads;
+    const int group = wave / SPLIT, part = wave % SPLIT * NB;            // its rows and, of a stage, its first block of keys
+    const int index = divide(blockIdx.x, a.by_kv), head = blockIdx.x - index * a.kv_heads;
     // the tiles with most keys first
-    const RowRange r = find_rows(a.starts, a.count, a.M, a.group, ROWS, 1, pieces - 1 - (int)(blockIdx.x / a.kv_heads));
+    const RowRange r = find_rows(a.starts, a.count, a.M, a.group, ROWS, 1, a.pieces - 1 - index);
     if (r.id < 0) return;
     const int all = r.n * a.group, row0 = r.piece * ROWS;
     if (row0 >= all) return;
     const int rows = min(ROWS, all - row0);
-    const int keys = (row0 + rows - 1) / a.group + 1;                    // that the last row sees
+    const int keys = divide(row0 + rows - 1, a.by_group) + 1;                    // that the last row sees
     const int stages = (keys + kKeys - 1) / kKeys;
     // this lane's row, and what its wavefront sees
-    const int row = row0 + min(32 * wave + i32, rows - 1), token = row / a.group;
-    const bool mine = 32 * wave + i32 < rows;
-    const int w_first = row0 + 32 * wave, w_last = row0 + min(32 * wave + 31, rows - 1);
-    const int sees_all = w_first / a.group, sees_any = 32 * wave < rows ? w_last / a.group : -1;
+    const int row = row0 + min(32 * group + i32, rows - 1), token = divide(row, a.by_group);
+    const bool mine = 32 * group + i32 < rows;
+    const int w_first = row0 + 32 * group, w_last = row0 + min(32 * group + 31, rows - 1);
+    const int sees_all = divide(w_first, a.by_group), sees_any = 32 * group < rows ? divide(w_last, a.by_group) : -1;
     const int q_head = head * a.group + row - token * a.group;
     v8h q[D / 16];
     {
@@ -149,62 +152,62 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
         wait_vmcnt<0>();
         lds_barrier();                           // everyone's loads of this stage are there, and everyone is done with the last one
         if (stage + 1 < stages) fetch(stage + 1, buf ^ 1);
-        const int first = stage * kKeys;
+        const int first = stage * kKeys + 32 * part;
         if (first > sees_any) continue;
-        const uint8_t *ks = lds[buf][0], *vs = lds[buf][1];
-        v16f s[2];
+        const uint8_t *ks = lds[buf][0] + 32 * part * LINE, *vs = lds[buf][1] + 32 * part * LINE;
+        v16f s[NB];
         {
             constexpr int AHEAD = 4;                 // operands asked for ahead of the instruction that takes them
             v8h ring[AHEAD];
-            auto key_part = [&](int n) {             // n: block n % 2, channels 16 (n / 2) ..
-                const int line = 32 * (n & 1) + i32;
-                return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * (((n & ~1) + half) ^ key_swizzle<D>(line)));
+            auto key_part = [&](int n) {             // n: block n % NB, channels 16 (n / NB) ..
+                const int line = 32 * (n % NB) + i32;
+                return *reinterpret_cast<const v8h *>(ks + line * LINE + 16 * ((2 * (n / NB) + half) ^ key_swizzle<D>(line)));
             };
 #pragma unroll
             for (int n = 0; n < AHEAD; ++n) ring[n] = key_part(n);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n) {
-                s[n & 1] = mfma_h(ring[n % AHEAD], q[n >> 1], s[n & 1]);
-                if (n + AHEAD < D / 8) ring[n % AHEAD] = key_part(n + AHEAD);
+            for (int n = 0; n < D / 16 * NB; ++n) {
+                s[n % NB] = mfma_h(ring[n % AHEAD], q[n / NB], s[n % NB]);
+                if (n + AHEAD < D / 16 * NB) ring[n % AHEAD] = key_part(n + AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (first + kKeys - 1 > sees_all) {
+        if (first + 32 * NB - 1 > sees_all) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (first + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) > token) s[b][i] = -INFINITY;
         }
-        v8h p[2][2];
-        float part;
+        v8h p[NB][2];
+        float total;
         auto weights = [&] {
             const float less = top - kShift;
-            part = 0.0f;
+            total = 0.0f;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
                     const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], a.scale, -less));
                     const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i + 1], a.scale, -less));
-                    part += e0;
-                    part += e1;
+                    total += e0;
+                    total += e1;
                     const v2h h = __builtin_convertvector((v2f{e0, e1}), v2h);
                     p[b][i / 8][i % 8] = h[0];
                     p[b][i / 8][i % 8 + 1] = h[1];
                 }
         };
-        weights();
-        if (__any(part > kMost)) {                   // a score far above m
+        if (stage != 0) weights();
+        if (stage == 0 || __any(total > kMost)) {    // a score far above m: at the first stage, all of them
             float x = s[0][0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) x = fmaxf(x, s[0][i]);
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x = fmaxf(x, s[1][i]);
+                for (int i = 0; i < 16; ++i) x = fmaxf(x, s[b][i]);
             auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
             const float next = fmaxf(top, fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * a.scale);
             const float f = __builtin_amdgcn_exp2f(top - next);
@@ -216,11 +219,11 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
                 for (int i = 0; i < 16; ++i) o[t][i] *= f;
             weights();
         }
-        sum += part;
+        sum += total;
         // lane (dsub, h) of sixteen lanes each: keys 4 h + 0 .. 3 (and 8 more on) of channels 16 dsub .. + 15
         const int h = lane >> 5, dsub = lane >> 4 & 1, e = lane >> 2 & 3, c4 = lane & 3;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -237,6 +240,33 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
                     }
                     o[t] = mfma_h(x.v, p[b][u], o[t]);
                 }
+    }
+    if constexpr (SPLIT == 2) {                        // the second wavefront's share to the first, lane by lane
+        constexpr int UNITS = D / 8, SHARE = (UNITS + 1) * 64;
+        v4f *share = reinterpret_cast<v4f *>(&lds[0][0][0]) + group * SHARE + lane;
+        static_assert(WAVES / SPLIT * SHARE * 16 <= (int)sizeof(lds), "shares fit into the stages' place");
+        lds_barrier();
+        if (part != 0) {
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    share[64 * (4 * t + i)] = v4f{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+            share[64 * UNITS] = v4f{top, sum, 0.0f, 0.0f};
+        }
+        lds_barrier();
+        if (part != 0) return;
+        const v4f other = share[64 * UNITS];
+        const float next = fmaxf(top, other[0]), f = __builtin_amdgcn_exp2f(top - next), g = __builtin_amdgcn_exp2f(other[0] - next);
+        sum = sum * f + other[1] * g;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v4f x = share[64 * (4 * t + i)];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][4 * i + e] = o[t][4 * i + e] * f + x[e] * g;
+            }
     }
     {
         auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
@@ -295,12 +325,24 @@ flexq_status flexq_prompt_attention(const uint16_t *q, int q_stride, const uint1
     // rows: 16384 tokens of 64 heads over 8 4280 / 4200, 8192 of 32 543 / 533, 4096 of 64 over 8 287 / 289; heads of 64, 16384
     // of 24 over 6, 873 / 940)
     const int waves = head_dim == 128 && (long)M * a.group / 256 * kv_heads >= 1024 ? 8 : 4;
-    const long grid = ((long)M * a.group / (32 * waves) + sequences) * kv_heads;
+    // Two wavefronts to 32 rows where there are too few for the chip and the longest chain of stages counts: a workgroup a CU or
+    // two, of long sequences (us with one / two: 512 tokens of 32 heads 14.3 / 12.2, 1500 37 / 34, of 8 heads over 1 5000 99 / 80;
+    // heads of 64, 2600 of 24 over 6 42 / 35; but 900 of 64 over 8, 450 workgroups, 28.0 / 29.7, 4 x 200 of 40 12.7 / 15.6)
+    const int split = waves == 4 && (long)M * a.group / 128 * kv_heads <= (head_dim == 64 ? 512 : 384) &&
+                      M >= (head_dim == 64 ? 256L : 512L) * sequences ? 2 : 1;
+    const int rows = 32 * waves / split;
+    const long pieces = (long)M * a.group / rows + sequences, grid = pieces * kv_heads;
     if (grid * 64 * waves >= (1L << 32)) return FLEXQ_ESHAPE;            // threads of a launch
+    a.pieces = (int)pieces;
+    a.by_group = divider(a.group);
+    a.by_kv = divider(kv_heads);
     auto launch = [&](auto kern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(64 * waves), 0, (hipStream_t)stream, a);
     };
-    head_dim == 64 ? launch(prompt_kernel<64, 4>) : waves == 4 ? launch(prompt_kernel<128, 4>) : launch(prompt_kernel<128, 8>);
+    if (head_dim == 64)
+        split == 2 ? launch(prompt_kernel<64, 4, 2>) : launch(prompt_kernel<64, 4, 1>);
+    else
+        waves == 8 ? launch(prompt_kernel<128, 8, 1>) : split == 2 ? launch(prompt_kernel<128, 4, 2>) : launch(prompt_kernel<128, 4, 1>);
     return hipGetLastError() == hipSuccess ? FLEXQ_OK : FLEXQ_EHIP;
 }
 

@@ -6,6 +6,12 @@
 
 namespace flexq {
 
+// Division by a number that the host knows: floor(2^32 / d) is at most one short in the quotient of x < 2^31.
+struct Divider {
+    unsigned d, magic;
+};
+inline Divider divider(int d) { return Divider{(unsigned)d, d == 1 ? 0xffffffffu : (unsigned)(0x100000000ull / (unsigned)d)}; }
+
 // A cache and the sequences of a call, as kernels take them.
 struct CacheArgs {
     uint8_t *codes;              // [pages][page_bytes]
@@ -13,6 +19,7 @@ struct CacheArgs {
     const int32_t *starts, *lengths, *table, *slots;
     size_t page_bytes;
     int kv_heads, pages, slot_count;
+    Divider by_kv;
     int shift;                   // blocks of a page: 1 << shift
     int count, max_pages, M;
 };
@@ -25,6 +32,8 @@ flexq_status cache_args(const flexq_cache *C, const flexq_sequences *S, int M, C
 namespace {
 
 using flexq::CacheArgs;
+using flexq::Divider;
+using flexq::divider;
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v4h __attribute__((ext_vector_type(4)));
@@ -33,6 +42,12 @@ typedef float v2f __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = FLEXQ_CACHE_BLOCK;    // tokens that share a scale
 constexpr int kCodeBias = 128;               // codes are stored as code + 128
+
+__device__ __forceinline__ int divide(int x, Divider by)
+{
+    const unsigned q = __umulhi((unsigned)x, by.magic);
+    return (int)(q + ((unsigned)x - q * by.d >= by.d ? 1u : 0u));
+}
 
 // The largest finite fp16 at most: the rounding of weights, or of a scale, may lead a mean of finite values beyond it.
 __device__ __forceinline__ float within_half(float y)

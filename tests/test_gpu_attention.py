@@ -94,7 +94,7 @@ def check_prompt(q, k, v, parts, heads, kv, got, scale):
 @pytest.mark.parametrize("heads,kv,D,parts", [
     (1, 1, 64, [1]), (1, 1, 128, [1]), (8, 1, 128, [1, 1, 1]), (4, 2, 64, [0, 5, 0, 0, 17, 1, 0]), (3, 1, 128, [63, 64, 65, 1, 129]),
     (5, 5, 64, [31, 33, 127, 128, 2]), (10, 2, 128, [300, 7, 211]), (2, 1, 64, [700]), (7, 1, 128, [260, 3]), (16, 1, 64, [90]),
-    (80, 2, 64, [40, 11]), (2, 2, 128, [512, 257, 1, 1])])
+    (80, 2, 64, [40, 11]), (2, 2, 128, [512, 257, 1, 1]), (4, 2, 128, [600]), (3, 1, 128, [515, 1000]), (6, 2, 64, [300, 212])])
 def test_prompt(heads, kv, D, parts):
     say(f"prompt heads={heads}/{kv} D={D} {parts}")
     rng = np.random.default_rng([heads, D, sum(parts)])
