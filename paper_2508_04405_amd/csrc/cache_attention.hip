@@ -15,7 +15,12 @@
 //
 // Work is cut evenly: all steps of all tiles of a key head lie in a row, and workgroup i of W takes the i-th part of them,
 // whatever sequences it meets there; a tile that several take leaves running maximum, sum and output of each in the
-// workspace and a second launch joins them in order.  A step's loads are 2 KiB a block and lane-contiguous.
+// workspace and a second launch joins them in order.  A step's loads are 2 KiB a block and lane-contiguous, a step ahead, and
+// non-temporal, since no one reads them again soon (48 sequences of up to 8192 tokens, 64 heads over 8: 87 -> 75 us).
+//
+// Bound by memory where the cache is long: those 413 MB in 74 us, 5.6 TB/s of the 6.5 that reads alone reach, one sequence of
+// 131072 tokens, 269 MB, in 48; and the joining launch, 3 to 5 us, which would want a wait between workgroups to go.  A short
+// cache takes the trips one after the other: lengths, table, codes, shares (1100 tokens of 32 heads 6.8 + 3.3 us).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
@@ -61,7 +66,7 @@ struct Steps {
         const int lane = threadIdx.x & 63, s = min(s0 + lane, a.c.count - 1);
         begin = max(a.c.starts[s], 0);
         end = min(a.c.starts[s + 1], a.c.M);
-        length = cached_length(a.c, s);
+        length = cached_length(a.c, a.c.lengths[s]);
         tiles = s0 + lane < a.c.count ? (max(end - begin, 0) * a.group + ROWS - 1) / ROWS : 0;
         steps = max((length + KEYS - 1) / KEYS, 1);
         const int sum = wave_scan(tiles * steps);
@@ -332,7 +337,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         };
         int s = first + wave;
         if (s < done) {
-            constexpr int N = 2;                         // (three or four: no faster)
+            constexpr int N = 2;                         // steps in registers (three or four: no faster)
             Stage<D> st[N];
             int page[N][2], next[2];
 #pragma unroll
@@ -438,9 +443,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 
 // Many rows: 128 of a tile, 32 a wavefront, and 64 keys a stage that all of them share.  The codes of the next stage are asked for
 // while this one is worked on, and put into LDS as fp16 behind it (two buffers), in the order in which the 32x32x16 MFMAs of the
-// prompts' kernel read them, so that a code is turned once for 128 rows.  A block of 16 keys is half of a result's
+// prompts' kernel read them, so that a code is turned once for 128 rows.  Heads of 64 take 128 keys a stage, for which LDS and
+// registers are there (three chunks of 400 tokens of 30 heads over 6, behind up to 9000: 90 -> 85 us).  A block of 16 keys is half of a result's
 // registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is raised only where a lane's weights of
 // a block add up to more than 2^15.
+//
+// Bound by the vector unit: 128 rows and 64 keys are 16 to 32 matrix instructions of 32 cycles a wavefront, beside about 250
+// vector ones of four (eight for an exponential), and two wavefronts a SIMD leave gaps in both (56 % and 23 % busy with heads of 64).
+// Codes put into LDS between the matrix instructions, not behind them: slower (95 -> 103 us, at 64 keys a stage).
 constexpr int kStageWaves = 4, kStageRows = 32 * kStageWaves;
 constexpr int stage_keys(int D) { return D == 64 ? 128 : 64; }
 constexpr float kStageShift = 9.0f, kMost = 32768.0f;
@@ -808,7 +818,9 @@ int tile_rows(int M, int count, int group)
     return rows > 64 ? kStageRows : rows > 16 ? 32 : 16;
 }
 
-// Workgroups of a key head: one a CU in all of the streaming kernel, two of the other.
+// Workgroups of a key head: one a CU in all of the streaming kernel, of eight wavefronts, two of the other.  (Streaming, 1 x 8
+// or 2 x 4 wavefronts a CU, us: 8 rows of 8192 tokens of 64 heads over 8 16.6 / 19.2, 16 sequences of 4000 45 / 60, 48 of up to 8192 80 /
+// 80; two tiles of 32 rows, 8 sequences of 4000 of 32 key heads, 99 / 81.)
 int parts_for(int kv_heads, int rows)
 {
     const int parts = (rows == kStageRows ? 512 : 256) / kv_heads;
@@ -863,6 +875,7 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     a.parts = parts_for(kv, rows);
     a.by_group = divider(a.group);
     a.by_parts = divider(a.parts);
+    // (a part of a few steps costs more in the join than it saves: 11 rows of 8192 tokens 21.5 us, with a step at least 27)
     a.least = rows == kStageRows ? 256 / stage_keys(D) : 8;
     const int groups = rows == kStageRows ? (most + 256 / D - 1) / (256 / D) : most;     // of rows of a tile
     if ((long)a.parts * kv * groups >= (1L << 26)) return FLEXQ_ESHAPE;  // 64 threads each, 2^32 a launch

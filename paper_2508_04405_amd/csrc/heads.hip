@@ -11,15 +11,17 @@
 // (freq / 2 pi), less the nearest quarter), so that a position of a million is as good as one of ten; what is left, an
 // eighth of a turn at most, goes through the Taylor series of sine and cosine, whose next terms are below 2^-28.
 //
-// Bound by memory (each row read and written once) where there are many, by the launch and two trips where there are few.
+// Bound by memory (each row read and written once) where there are many, by the launch and two trips where there are few: 4096 tokens
+// of 64 + 8 heads of 128 take 28 us, 5.3 TB/s, with norms or without, one token 2.1 us.  A token's heads are spread over as many
+// workgroups as they fill, each of which makes the angles; four tokens in one workgroup, which makes them once: 512 tokens 6.0 -> 11.4
+// us, 4096 25.5 -> 28.7, 8192 50 -> 52.5.
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
 #include "producer_math.h"
+#include "sequences.h"
 
 namespace {
-
-constexpr int kMostTokens = 4;               // of a workgroup
 
 struct RotateArgs {
     const uint16_t *x, *gamma_q, *gamma_k;
@@ -28,8 +30,8 @@ struct RotateArgs {
     const float *freq;
     size_t x_stride, out_stride;
     int M, heads, all;                       // all: heads and key heads
-    int rot, tokens, chunks;                 // tokens of a workgroup; workgroups that share them
-    unsigned magic;                          // floor(u / per) = (u * magic) >> 32
+    int rot;
+    Divider by_chunks;                       // workgroups of a token
     float eps;
 };
 
@@ -49,63 +51,57 @@ template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
 {
     constexpr int LH = D / 16;               // lanes of a head
-    __shared__ float2 angles[kMostTokens][D / 2];
-    const int m0 = blockIdx.x / p.chunks * p.tokens, chunk = blockIdx.x % p.chunks;
-    const int tokens = min(p.tokens, p.M - m0), half = p.rot / 2;
-    for (int i = threadIdx.x; i < tokens * (D / 2); i += 256) {
-        const int t = i / (D / 2), f = i % (D / 2);
-        if (f < half) angles[t][f] = turn(p.positions[m0 + t], p.freq[f]);
-    }
-    __syncthreads();
-    const int per = p.all * LH, units = tokens * per;
+    __shared__ float2 angles[D / 2];
+    const int m = divide(blockIdx.x, p.by_chunks), chunk = blockIdx.x - m * (int)p.by_chunks.d, half = p.rot / 2;
     const int lane = threadIdx.x % LH, pairs = p.rot / 16;       // the first `pairs` lanes of a head rotate
     const bool rotates = lane < pairs;
     const int a0 = !rotates || INTERLEAVED ? 16 * lane : 8 * lane;
     const int b0 = !rotates || INTERLEAVED ? a0 + 8 : half + 8 * lane;
-    for (int u = chunk * 256 + threadIdx.x; u < units; u += p.chunks * 256) {
-        const int t = (int)__umulhi((unsigned)u, p.magic), head = (u - t * per) / LH;
-        const uint16_t *x = p.x + (size_t)(m0 + t) * p.x_stride + (size_t)head * D;
-        const uint4 va = *reinterpret_cast<const uint4 *>(x + a0), vb = *reinterpret_cast<const uint4 *>(x + b0);
-        const unsigned w[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
-        float v[16];
+    const int head = (chunk * 256 + (int)threadIdx.x) / LH;
+    const uint16_t *x = p.x + (size_t)m * p.x_stride + (size_t)min(head, p.all - 1) * D;     // (on the way while the angles are made)
+    const uint4 va = *reinterpret_cast<const uint4 *>(x + a0), vb = *reinterpret_cast<const uint4 *>(x + b0);
+    if ((int)threadIdx.x < half) angles[threadIdx.x] = turn(p.positions[m], p.freq[threadIdx.x]);
+    __syncthreads();
+    if (head >= p.all) return;
+    const unsigned w[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[2 * i] = h2f((uint16_t)(w[i] & 0xffffu));
+        v[2 * i + 1] = h2f((uint16_t)(w[i] >> 16));
+    }
+    const uint16_t *gamma = head < p.heads ? p.gamma_q : p.gamma_k;
+    if (gamma) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
+#pragma unroll
+        for (int d = 1; d < LH; d <<= 1) ss += __shfl_xor(ss, d, 64);
+        const float inv = __builtin_amdgcn_rsqf(ss * (1.0f / D) + p.eps);
+        const uint4 ga = *reinterpret_cast<const uint4 *>(gamma + a0), gb = *reinterpret_cast<const uint4 *>(gamma + b0);
+        const unsigned g[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            v[2 * i] = h2f((uint16_t)(w[i] & 0xffffu));
-            v[2 * i + 1] = h2f((uint16_t)(w[i] >> 16));
+            v[2 * i] = v[2 * i] * inv * h2f((uint16_t)(g[i] & 0xffffu));
+            v[2 * i + 1] = v[2 * i + 1] * inv * h2f((uint16_t)(g[i] >> 16));
         }
-        const uint16_t *gamma = head < p.heads ? p.gamma_q : p.gamma_k;
-        if (gamma) {
-            float ss = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
-#pragma unroll
-            for (int d = 1; d < LH; d <<= 1) ss += __shfl_xor(ss, d, 64);
-            const float inv = __builtin_amdgcn_rsqf(ss * (1.0f / D) + p.eps);
-            const uint4 ga = *reinterpret_cast<const uint4 *>(gamma + a0), gb = *reinterpret_cast<const uint4 *>(gamma + b0);
-            const unsigned g[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[2 * i] = v[2 * i] * inv * h2f((uint16_t)(g[i] & 0xffffu));
-                v[2 * i + 1] = v[2 * i + 1] * inv * h2f((uint16_t)(g[i] >> 16));
-            }
-        }
-        if (rotates) {
-            const float2 *angle = &angles[t][8 * lane];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = angle[i].x, s = angle[i].y;
-                float &first = v[INTERLEAVED ? 2 * i : i], &second = v[INTERLEAVED ? 2 * i + 1 : 8 + i];
-                const float a = first, b = second;
-                first = a * c - b * s;
-                second = b * c + a * s;
-            }
-        }
-        uint16_t *out = p.out + (size_t)(m0 + t) * p.out_stride + (size_t)head * D;
-        *reinterpret_cast<uint4 *>(out + a0) =
-            make_uint4(pack_h2(v[0], v[1]), pack_h2(v[2], v[3]), pack_h2(v[4], v[5]), pack_h2(v[6], v[7]));
-        *reinterpret_cast<uint4 *>(out + b0) =
-            make_uint4(pack_h2(v[8], v[9]), pack_h2(v[10], v[11]), pack_h2(v[12], v[13]), pack_h2(v[14], v[15]));
     }
+    if (rotates) {
+        const float2 *angle = &angles[8 * lane];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = angle[i].x, s = angle[i].y;
+            float &first = v[INTERLEAVED ? 2 * i : i], &second = v[INTERLEAVED ? 2 * i + 1 : 8 + i];
+            const float a = first, b = second;
+            first = a * c - b * s;
+            second = b * c + a * s;
+        }
+    }
+    uint16_t *out = p.out + (size_t)m * p.out_stride + (size_t)head * D;
+    *reinterpret_cast<uint4 *>(out + a0) =
+        make_uint4(pack_h2(v[0], v[1]), pack_h2(v[2], v[3]), pack_h2(v[4], v[5]), pack_h2(v[6], v[7]));
+    *reinterpret_cast<uint4 *>(out + b0) =
+        make_uint4(pack_h2(v[8], v[9]), pack_h2(v[10], v[11]), pack_h2(v[12], v[13]), pack_h2(v[14], v[15]));
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -144,11 +140,9 @@ flexq_status flexq_rotate_heads(const uint16_t *x, int x_stride, int M, int head
     p.all = heads + kv_heads;
     p.rot = rot;
     p.eps = eps;
-    const int per = p.all * (head_dim / 16);
-    p.tokens = M >= 2048 ? kMostTokens : 1;
-    p.chunks = M >= 2048 ? 1 : (per + 255) / 256;
-    p.magic = (unsigned)((0x100000000ull + per - 1) / per);      // exact below 2^32 / per, and units are at most 4 * per
-    const long grid = ((long)M + p.tokens - 1) / p.tokens * p.chunks;
+    const int chunks = (p.all * (head_dim / 16) + 255) / 256;
+    p.by_chunks = divider(chunks);
+    const long grid = (long)M * chunks;
     if (grid >= (1L << 24)) return FLEXQ_ESHAPE;                 // 256 threads each, 2^32 a launch
     auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, p); };
     if (head_dim == 128)

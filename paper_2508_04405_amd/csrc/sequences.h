@@ -58,13 +58,15 @@ __device__ __forceinline__ float within_half(float y)
 struct RowRange {
     int id, begin, n;    // sequence (-1: none), its first row, its rows
     int piece;           // number of the piece within the sequence
+    int length;          // lengths[id], where lengths are given
 };
 
 // Sequence s owns pieces place(s) .. place(s + 1) - 1 of a launch, place(s) = floor(starts[s] * mul / div) + extra * s: a
 // closed form that leaves every sequence as many as it can need -- ceil(n mul / div) of them with extra = 1 -- so that no
 // one adds up the lengths of those before.  Whose piece `index` is, is the last s with place(s) <= index; every wavefront
 // finds it for itself, 64 sequences a step.  starts outside 0 .. rows, or falling, never lead outside the rows.
-__device__ __forceinline__ RowRange find_rows(const int32_t *starts, int count, int rows, int mul, int div, int extra, int index)
+__device__ __forceinline__ RowRange find_rows(const int32_t *starts, int count, int rows, int mul, int div, int extra, int index,
+                                              const int32_t *lengths = nullptr)
 {
     const int lane = threadIdx.x & 63;
     auto start = [&](int s) { return min(max(starts[s], 0), rows); };
@@ -74,19 +76,20 @@ __device__ __forceinline__ RowRange find_rows(const int32_t *starts, int count, 
         const int step = (span + 63) / 64, s = lo + lane * step;
         const bool before = lane * step < span && place(start(min(s, count)), s) <= index;
         const int hits = __builtin_popcountll(__ballot(before));
-        if (hits == 0) return RowRange{-1, 0, 0, 0};
+        if (hits == 0) return RowRange{-1, 0, 0, 0, 0};
         lo += (hits - 1) * step;
         span = min(step, span - (hits - 1) * step);
     }
     const int s = min(lo + lane, count - 1), a = start(s), b = max(start(s + 1), a);
-    const int p = place(a, s);
+    const int p = place(a, s), length = lengths ? lengths[s] : 0;
     const int hits = __builtin_popcountll(__ballot(lane < span && p <= index));
-    if (hits == 0) return RowRange{-1, 0, 0, 0};
+    if (hits == 0) return RowRange{-1, 0, 0, 0, 0};
     RowRange r;
     r.id = lo + hits - 1;
     r.begin = __builtin_amdgcn_readlane(a, hits - 1);
     r.n = __builtin_amdgcn_readlane(b, hits - 1) - r.begin;
     r.piece = index - __builtin_amdgcn_readlane(p, hits - 1);
+    r.length = __builtin_amdgcn_readlane(length, hits - 1);
     return r;
 }
 
@@ -140,9 +143,9 @@ struct CacheBlock {
     }
 };
 
-__device__ __forceinline__ int cached_length(const CacheArgs &c, int s)
+__device__ __forceinline__ int cached_length(const CacheArgs &c, int length)
 {
-    return min(max(c.lengths[s], 0), c.max_pages << (c.shift + 4));
+    return min(max(length, 0), c.max_pages << (c.shift + 4));
 }
 
 }  // namespace
