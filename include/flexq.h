@@ -299,7 +299,7 @@ flexq_status flexq_linear_g128(const void *packed, const int8_t *xq,
  *
  * Attention itself and the residual additions are not part of this path: the caller
  * supplies the attention output `attn` and the input of the second norm `x_ffn` (it
- * may alias `o`), and may run the stages in two calls around its own attention with
+ * may alias `o`), and may run the stages in two calls around attention (below) with
  * first_stage / last_stage (0 <= first_stage <= last_stage <= 3).
  *
  * flexq_layer: H hidden size, F feed-forward width, QKV width of the fused QKV
@@ -478,7 +478,11 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  * head_dim is 64 or 128; `heads` query heads share kv_heads key heads, heads / kv_heads each, in order.  Rows are fp16, one
  * a token, their heads one after the other; a row stride counts elements, is a multiple of 8 and at least the row's width,
  * so that the parts of a fused QKV row are taken where they lie.  Pointers to rows are 16-byte aligned, and what is written
- * overlaps no input unless it says so.  Inputs are finite (rows that belong to no sequence may hold anything).
+ * overlaps no input unless it says so.  Inputs are finite (rows that belong to no sequence may hold anything): a token that is
+ * not may reach others of its sequence, earlier ones too.  Attention gives finite values, 65504 at most.  FLEXQ_ESHAPE is also what
+ * is beyond the kernels' indices: heads * head_dim above FLEXQ_MAX_K, M * heads / kv_heads of 2^30 and more, more than 2^20
+ * sequences, a table of more than 2^30 tokens, more than 2^23 as a stride of prompts' k or v, and over the cache
+ * (M * heads / kv_heads / 16 + count) * (max_pages * page / 32 + 1) of 2^31 and more.
  *
  * flexq_rotate_heads: heads of queries, then of keys, in the first (heads + kv_heads) * head_dim columns of x:
  *   h = x / sqrt(mean(x^2) + eps) * gamma over each head (gamma_q, gamma_k dev, fp16 [head_dim], 16-byte aligned; NULL: h = x),
@@ -504,7 +508,7 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  *   codes    dev, 16-byte aligned, pages * flexq_cache_page_bytes(...) bytes: pages are copied and moved as they are
  *   recent   dev, 16-byte aligned, slots * flexq_cache_recent_bytes(...) bytes: slots likewise
  * Neither needs to be initialised.  flexq_sequences, beside starts (the batch's rows are the sequences' newest tokens):
- *   lengths  dev, int32 [count]: tokens of each sequence, the batch's among them
+ *   lengths  dev, int32 [count]: tokens of each sequence, the batch's among them; beyond what its table has room for, that much
  *   table    dev, int32 [count][max_pages]: its pages in order.  What a page outside 0 .. pages - 1 would hold is not there:
  *            appends drop it, attention does not see it, reads give zero.  Entries behind the length are not looked at
  *   slots    dev, int32 [count], its slot, different ones; outside 0 .. slots - 1 likewise.  NULL: sequence i has slot i
