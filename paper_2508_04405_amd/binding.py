@@ -632,7 +632,7 @@ def _rows(t, rows, width, dev, exact=True):
             or t.stride(1) != 1):
         raise FlexQError(f"flexq: expected fp16 rows [{rows}, {width}] on the current device, got {t.dtype} {list(s)} of strides "
                          f"{list(t.stride())} on {t.device}")
-    return t.stride(0) if rows > 1 else max(t.stride(0), (s[1] + 7) // 8 * 8)
+    return t.stride(0) if rows > 1 else (s[1] + 7) // 8 * 8
 
 
 def _head_dim(t, heads):

@@ -90,6 +90,7 @@ __device__ __forceinline__ RowRange find_rows(const int32_t *starts, int count, 
     r.n = __builtin_amdgcn_readlane(b, hits - 1) - r.begin;
     r.piece = index - __builtin_amdgcn_readlane(p, hits - 1);
     r.length = __builtin_amdgcn_readlane(length, hits - 1);
+    if (r.piece < 0) r.id = -1;                          // (falling starts)
     return r;
 }
 

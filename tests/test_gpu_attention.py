@@ -295,7 +295,7 @@ def test_a_sequence_can_be_shortened():
     (8, 2, 64, 32, [1, 15, 16, 17, 31, 32, 33, 300], [1] * 8), (40, 8, 128, 128, [129, 3, 700], [1, 1, 1]),
     (24, 6, 64, 16, [50, 60, 400, 5], [4, 0, 8, 5]), (5, 1, 128, 32, [900, 200, 64], [3, 7, 64]),
     (16, 2, 64, 64, [333, 1000], [100, 300]), (16, 1, 128, 16, [2100], [130]), (34, 2, 128, 16, [40, 500], [1, 1]),
-    (3, 3, 64, 1024, [3000, 2049], [1, 2])])
+    (3, 3, 64, 1024, [3000, 2049], [1, 2]), (200, 1, 64, 16, [150], [1]), (70, 1, 128, 32, [90, 33], [1, 0])])
 def test_cached_attention(heads, kv, D, page, lengths, new):
     say(f"cached heads={heads}/{kv} D={D} page={page} {lengths} {new}")
     rng = np.random.default_rng([heads, D, page, sum(lengths)])
@@ -371,6 +371,39 @@ def test_chunks_that_see_nothing_or_not_all(D):
     out = run(scale=1.4e-45)
     for rows, i, first in ((slice(0, 40), 0, 60), (slice(40, 70), 1, 80), (slice(70, 80), 2, 90)):
         check(out, rows, k[i], v[i], first, 1.4e-45)
+
+
+def test_starts_that_fall_or_lie_outside():
+    """What they do not describe is left out or wrong; what they describe is right, and rows outside stay as they were."""
+    rng = np.random.default_rng(25)
+    kv, D, heads, M = 2, 64, 16, 100
+    q, k, v = normal(rng, M, heads * D), keys(rng, M, kv * D), normal(rng, M, kv * D)
+    s = Story(rng, 3, kv, D, 16, 160)
+    s.append([30, 40, 50])
+    for starts in ([0, 50, 20, 500], [-7, 10, 10, 60], [60, 60, 2**31 - 1, 3], [0, -2**31, 70, 90]):
+        say(f"starts {starts}")
+        out = torch.full((M + 8, heads * D), 5.0, dtype=torch.float16, device=DEV)
+        fq.prompt_attention(to_dev(q), to_dev(k), to_dev(v), heads, kv, i32(starts), out=out[:M])
+        got = host(out)
+        assert np.isfinite(got).all() and (got[M:] == 5.0).all()
+        if starts[0] == -7:
+            for lo, hi in ((0, 10), (10, 60)):
+                check_prompt(q[lo:hi], k[lo:hi], v[lo:hi], [hi - lo], heads, kv, got[lo:hi], D ** -0.5)
+            assert (got[60:] == 5.0).all()
+        seqs = fq.Sequences(i32(starts), i32(s.lengths()), to_dev(s.table), to_dev(s.slots))
+        out.fill_(5.0)
+        fq.cache_attention(s.cache, to_dev(q), heads, seqs, out=out[:M])
+        got = host(out)
+        assert np.isfinite(got).all() and (got[M:] == 5.0).all()
+        back = torch.full((2, M + 8, kv * D), 5.0, dtype=torch.float16, device=DEV)
+        fq.cache_read(s.cache, seqs, out=(back[0, :M], back[1, :M]))
+        assert (host(back)[:, M:] == 5.0).all()
+        pages = torch.full_like(s.cache.codes, 7)
+        copy = fq.Cache(*s.cache.codes.shape[:1], 16, kv, D, s.cache.slots)
+        copy.codes.copy_(pages)
+        fq.cache_append(copy, to_dev(k), to_dev(v), seqs)
+        unused = sorted(set(range(pages.shape[0])) - set(s.table.ravel().tolist()))
+        assert torch.equal(copy.codes[unused], pages[unused])
 
 
 def test_a_length_beyond_the_table_counts_as_its_end():
