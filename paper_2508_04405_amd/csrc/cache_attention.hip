@@ -809,18 +809,19 @@ __global__ __launch_bounds__(64) void join_kernel(CachedArgs a, Divider by_group
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Rows of a tile: as many as a sequence has on average; 128, which go through LDS, from 65 on, where tiles of 32 would read
-// the cache three times (us with 32 / 128 a tile: 64 rows, 16 sequences of 1000 tokens of 8 key heads 21.8 / 34, of 4000 46 / 60;
-// 65 rows, 40 of 2000 of 6 heads of 64 61 / 43; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
-int tile_rows(int M, int count, int group)
+// Rows of a tile: as many as a sequence has on average; 128, which go through LDS, where tiles of 32 would read the cache three times,
+// and with heads of 64 twice (us with 32 / 128 a tile: heads of 128, 64 rows, 16 sequences of 1000 tokens of 8 key heads 20.5 / 30, of
+// 4000 45 / 53, 8 of 4000 of 32 96 / 85, 72 rows, 16 of 4000 of 8, 85 / 56; heads of 64, 35 rows, 40 of 2000 of 6, 42.5 / 34.8, 50 rows, 10
+// of 3000 of 12, 35 / 32; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
+int tile_rows(int M, int count, int group, int head_dim)
 {
     const long rows = (long)M * group / count;
-    return rows > 64 ? kStageRows : rows > 16 ? 32 : 16;
+    return rows > (head_dim == 64 ? 32 : 64) ? kStageRows : rows > 16 ? 32 : 16;
 }
 
 // Workgroups of a key head: one a CU in all of the streaming kernel, of eight wavefronts, two of the other.  (Streaming, 1 x 8
 // or 2 x 4 wavefronts a CU, us: 8 rows of 8192 tokens of 64 heads over 8 16.6 / 19.2, 16 sequences of 4000 45 / 60, 48 of up to 8192 80 /
-// 80; two tiles of 32 rows, 8 sequences of 4000 of 32 key heads, 99 / 81.)
+// 80; two tiles of 32 rows each, 8 sequences of 4000 of 32 key heads, 99 / 81.)
 int parts_for(int kv_heads, int rows)
 {
     const int parts = (rows == kStageRows ? 512 : 256) / kv_heads;
@@ -829,7 +830,7 @@ int parts_for(int kv_heads, int rows)
 
 size_t workspace_for(int M, int count, int heads, int kv_heads, int head_dim)
 {
-    const int rows = tile_rows(M, count, heads / kv_heads);
+    const int rows = tile_rows(M, count, heads / kv_heads, head_dim);
     return (size_t)parts_for(kv_heads, rows) * kv_heads * 2 * rows * (head_dim + 4) * 4;
 }
 
@@ -871,7 +872,7 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     a.scale = scale * 1.44269504088896341f;
     a.group = heads / kv;
     a.heads = heads;
-    const int rows = tile_rows(M, seqs->count, a.group), most = (long)M * a.group < rows ? M * a.group : rows;
+    const int rows = tile_rows(M, seqs->count, a.group, D), most = (long)M * a.group < rows ? M * a.group : rows;
     a.parts = parts_for(kv, rows);
     a.by_group = divider(a.group);
     a.by_parts = divider(a.parts);

@@ -295,7 +295,7 @@ def test_a_sequence_can_be_shortened():
     (8, 2, 64, 32, [1, 15, 16, 17, 31, 32, 33, 300], [1] * 8), (40, 8, 128, 128, [129, 3, 700], [1, 1, 1]),
     (24, 6, 64, 16, [50, 60, 400, 5], [4, 0, 8, 5]), (5, 1, 128, 32, [900, 200, 64], [3, 7, 64]),
     (16, 2, 64, 64, [333, 1000], [100, 300]), (16, 1, 128, 16, [2100], [130]), (34, 2, 128, 16, [40, 500], [1, 1]),
-    (3, 3, 64, 1024, [3000, 2049], [1, 2]), (200, 1, 64, 16, [150], [1]), (70, 1, 128, 32, [90, 33], [1, 0])])
+    (3, 3, 64, 1024, [3000, 2049], [1, 2]), (200, 1, 64, 16, [150], [1]), (12, 3, 64, 32, [400, 77, 150], [9, 12, 10]), (12, 3, 128, 32, [400, 77, 150], [9, 12, 10]), (70, 1, 128, 32, [90, 33], [1, 0])])
 def test_cached_attention(heads, kv, D, page, lengths, new):
     say(f"cached heads={heads}/{kv} D={D} page={page} {lengths} {new}")
     rng = np.random.default_rng([heads, D, page, sum(lengths)])
