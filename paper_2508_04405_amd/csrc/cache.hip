@@ -6,12 +6,13 @@
 // rounded once, whatever way its block filled up, and the ring still holds the block before the unfinished one, to which a
 // sequence may be shortened.
 //
-// A workgroup takes one block of a sequence and head, its codes through LDS so that they go out 16 bytes a thread; the one that has a sequence's first block -- the only one that reads
-// tokens from the ring -- also writes the new tokens of its last two into the ring, after it has read.
+// A workgroup takes one block of a sequence and head, its codes through LDS so that they go out 16 bytes a thread; the one that
+// has a sequence's first block -- the only one that reads tokens from the ring -- also writes the new tokens of its last two
+// into the ring, after it has read.
 //
 // Bound by memory where there are many tokens: 4 bytes of rows in and 2 of codes out for each pair of elements; by the launch
-// and three dependent trips (starts, lengths, rows) where there are few.  5900 tokens of 40 heads of 128: 48 us in, 3.8 TB/s -- each
-// workgroup makes its trips for 12 KiB -- and 33 us out, 5.5 TB/s; a token of 32 sequences 4.9 and 3.4 us.
+// and three dependent trips (starts, lengths, rows) where there are few.  5900 tokens of 40 heads of 128: 47 us in, 3.9 TB/s --
+// each workgroup makes its trips for 12 KiB -- and 32 us out, 5.6 TB/s; a token of 32 sequences 4.9 and 3.4 us.
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
@@ -94,8 +95,9 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs a)
                     kv[i] = *reinterpret_cast<const uint4 *>(recent + B::recent_key(t, dk));
             }
         }
-        unsigned most = values ? max_bits(make_uint4(vv[2].x, vv[2].y, vv[3].x, vv[3].y), max_bits(make_uint4(vv[0].x, vv[0].y, vv[1].x, vv[1].y), 0u))
-                               : max_bits(kv[1], max_bits(kv[0], 0u));
+        const uint4 half0 = values ? make_uint4(vv[0].x, vv[0].y, vv[1].x, vv[1].y) : kv[0];
+        const uint4 half1 = values ? make_uint4(vv[2].x, vv[2].y, vv[3].x, vv[3].y) : kv[1];
+        unsigned most = max_bits(half1, max_bits(half0, 0u));
         most = wave_max_bits(most);
         if ((tid & 63) == 0) top[tid >> 6] = most;
         __syncthreads();

@@ -41,7 +41,7 @@ struct CachedArgs {
     size_t q_stride, out_stride;
     float *part;                                 // [kv_heads][parts][2][rows of a tile][D + 4]: output, running maximum, sum
     float scale;                                 // times log2 e
-    int group, heads, parts;                     // heads of a key head; workgroups of a key head
+    int group, parts;                            // heads of a key head; workgroups of a key head
     Divider by_group, by_parts;
     int least;                                   // steps that a workgroup takes at least
 };
@@ -441,16 +441,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-// Many rows: 128 of a tile, 32 a wavefront, and 64 keys a stage that all of them share.  The codes of the next stage are asked for
-// while this one is worked on, and put into LDS as fp16 behind it (two buffers), in the order in which the 32x32x16 MFMAs of the
-// prompts' kernel read them, so that a code is turned once for 128 rows.  Heads of 64 take 128 keys a stage, for which LDS and
-// registers are there (three chunks of 400 tokens of 30 heads over 6, behind up to 9000: 90 -> 85 us).  A block of 16 keys is half of a result's
-// registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is raised only where a lane's weights of
-// a block add up to more than 2^15.
+// Many rows: 128 of a tile, 32 a wavefront, and 64 keys a stage that all of them share.  The codes of the next stage are asked
+// for while this one is worked on, and put into LDS as fp16 behind it (two buffers), in the order in which the 32x32x16 MFMAs
+// of the prompts' kernel read them, so that a code is turned once for 128 rows.  Heads of 64 take 128 keys a stage, for which
+// LDS and registers are there (three chunks of 400 tokens of 30 heads over 6, behind up to 9000: 90 -> 85 us).  A block of 16
+// keys is half of a result's registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is
+// raised only where a lane's weights of a block add up to more than 2^15.
 //
 // Bound by the vector unit: 128 rows and 64 keys are 16 to 32 matrix instructions of 32 cycles a wavefront, beside about 250
-// vector ones of four (eight for an exponential), and two wavefronts a SIMD leave gaps in both (56 % and 23 % busy with heads of 64).
-// Codes put into LDS between the matrix instructions, not behind them: slower (95 -> 103 us, at 64 keys a stage).
+// vector ones of four (eight for an exponential), and two wavefronts a SIMD leave gaps in both (56 % and 23 % busy with heads
+// of 64). Codes put into LDS between the matrix instructions, not behind them: slower (95 -> 103 us, at 64 keys a stage).
 constexpr int kStageWaves = 4, kStageRows = 32 * kStageWaves;
 constexpr int stage_keys(int D) { return D == 64 ? 128 : 64; }
 constexpr float kStageShift = 9.0f, kMost = 32768.0f;
@@ -809,10 +809,10 @@ __global__ __launch_bounds__(64) void join_kernel(CachedArgs a, Divider by_group
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Rows of a tile: as many as a sequence has on average; 128, which go through LDS, where tiles of 32 would read the cache three times,
-// and with heads of 64 twice (us with 32 / 128 a tile: heads of 128, 64 rows, 16 sequences of 1000 tokens of 8 key heads 20.5 / 30, of
-// 4000 45 / 53, 8 of 4000 of 32 96 / 85, 72 rows, 16 of 4000 of 8, 85 / 56; heads of 64, 35 rows, 40 of 2000 of 6, 42.5 / 34.8, 50 rows, 10
-// of 3000 of 12, 35 / 32; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
+// Rows of a tile: as many as a sequence has on average; 128, which go through LDS, where tiles of 32 would read the cache three
+// times, and with heads of 64 twice (us with 32 / 128 a tile: heads of 128, 64 rows, 16 sequences of 1000 tokens of 8 key heads
+// 20.5 / 30, of 4000 45 / 53, 8 of 4000 of 32 96 / 85, 72 rows, 16 of 4000 of 8, 85 / 56; heads of 64, 35 rows, 40 of 2000 of
+// 6, 42.5 / 34.8, 50 rows, 10 of 3000 of 12, 35 / 32; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
 int tile_rows(int M, int count, int group, int head_dim)
 {
     const long rows = (long)M * group / count;
@@ -820,8 +820,8 @@ int tile_rows(int M, int count, int group, int head_dim)
 }
 
 // Workgroups of a key head: one a CU in all of the streaming kernel, of eight wavefronts, two of the other.  (Streaming, 1 x 8
-// or 2 x 4 wavefronts a CU, us: 8 rows of 8192 tokens of 64 heads over 8 16.6 / 19.2, 16 sequences of 4000 45 / 60, 48 of up to 8192 80 /
-// 80; two tiles of 32 rows each, 8 sequences of 4000 of 32 key heads, 99 / 81.)
+// or 2 x 4 wavefronts a CU, us: 8 rows of 8192 tokens of 64 heads over 8 16.6 / 19.2, 16 sequences of 4000 45 / 60, 48 of up to
+// 8192 80 / 80; two tiles of 32 rows each, 8 sequences of 4000 of 32 key heads, 99 / 81.)
 int parts_for(int kv_heads, int rows)
 {
     const int parts = (rows == kStageRows ? 512 : 256) / kv_heads;
@@ -871,7 +871,6 @@ flexq_status flexq_cache_attention(const flexq_cache *cache, const flexq_sequenc
     a.part = (float *)workspace;
     a.scale = scale * 1.44269504088896341f;
     a.group = heads / kv;
-    a.heads = heads;
     const int rows = tile_rows(M, seqs->count, a.group, D), most = (long)M * a.group < rows ? M * a.group : rows;
     a.parts = parts_for(kv, rows);
     a.by_group = divider(a.group);

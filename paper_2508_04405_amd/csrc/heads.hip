@@ -11,10 +11,10 @@
 // (freq / 2 pi), less the nearest quarter), so that a position of a million is as good as one of ten; what is left, an
 // eighth of a turn at most, goes through the Taylor series of sine and cosine, whose next terms are below 2^-28.
 //
-// Bound by memory (each row read and written once) where there are many, by the launch and two trips where there are few: 4096 tokens
-// of 64 + 8 heads of 128 take 28 us, 5.3 TB/s, with norms or without, one token 2.1 us.  A token's heads are spread over as many
-// workgroups as they fill, each of which makes the angles; four tokens in one workgroup, which makes them once: 512 tokens 6.0 -> 11.4
-// us, 4096 25.5 -> 28.7, 8192 50 -> 52.5.
+// Bound by memory (each row read and written once) where there are many, by the launch and two trips where there are few: 4096
+// tokens of 64 + 8 heads of 128 take 28 us, 5.3 TB/s, with norms or without, one token 2.1 us.  A token's heads are spread over
+// as many workgroups as they fill, each of which makes the angles; four tokens in one workgroup, which makes them once: 512
+// tokens 6.0 -> 11.4 us, 4096 25.5 -> 28.7, 8192 50 -> 52.5.
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
@@ -29,7 +29,7 @@ struct RotateArgs {
     const int32_t *positions;
     const float *freq;
     size_t x_stride, out_stride;
-    int M, heads, all;                       // all: heads and key heads
+    int heads, all;                          // all: heads and key heads
     int rot;
     Divider by_chunks;                       // workgroups of a token
     float eps;
@@ -58,7 +58,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
     const int a0 = !rotates || INTERLEAVED ? 16 * lane : 8 * lane;
     const int b0 = !rotates || INTERLEAVED ? a0 + 8 : half + 8 * lane;
     const int head = (chunk * 256 + (int)threadIdx.x) / LH;
-    const uint16_t *x = p.x + (size_t)m * p.x_stride + (size_t)min(head, p.all - 1) * D;     // (on the way while the angles are made)
+    const uint16_t *x = p.x + (size_t)m * p.x_stride + (size_t)min(head, p.all - 1) * D;
+    // (on their way while the angles are made)
     const uint4 va = *reinterpret_cast<const uint4 *>(x + a0), vb = *reinterpret_cast<const uint4 *>(x + b0);
     if ((int)threadIdx.x < half) angles[threadIdx.x] = turn(p.positions[m], p.freq[threadIdx.x]);
     __syncthreads();
@@ -135,7 +136,6 @@ flexq_status flexq_rotate_heads(const uint16_t *x, int x_stride, int M, int head
     p.freq = freq;
     p.x_stride = (size_t)x_stride;
     p.out_stride = (size_t)out_stride;
-    p.M = M;
     p.heads = heads;
     p.all = heads + kv_heads;
     p.rot = rot;
