@@ -15,7 +15,9 @@
 //
 // Work is cut evenly: all steps of all tiles of a key head lie in a row, and workgroup i of W takes the i-th part of them,
 // whatever sequences it meets there; a tile that several take leaves running maximum, sum and output of each in the
-// workspace and a second launch joins them in order.  A step's loads are 2 KiB a block and lane-contiguous, a step ahead, and
+// workspace and a second launch joins them in order.  Where there are many tiles of few steps, which would leave a workgroup's
+// wavefronts waiting for one another at every tile, each wavefront takes whole tiles of its own instead (`tiles_alone`: 58
+// sequences of up to 394 tokens of 32 key heads 56 -> 26 us, 38 of up to 23 of 8 36 -> 10, 64 of 1000 of 8 63 -> 49).  A step's loads are 2 KiB a block and lane-contiguous, a step ahead, and
 // non-temporal, since no one reads them again soon (48 sequences of up to 8192 tokens, 64 heads over 8: 87 -> 75 us).
 //
 // Bound by memory where the cache is long: those 413 MB in 74 us, 5.6 TB/s of the 6.5 that reads alone reach, one sequence of
@@ -43,7 +45,7 @@ struct CachedArgs {
     float scale;                                 // times log2 e
     int group, parts;                            // heads of a key head; workgroups of a key head
     Divider by_group, by_parts;
-    int least;                                   // steps that a workgroup takes at least
+    int least;                                   // steps that a workgroup takes at least, if a tile has them
 };
 
 // Where the steps of a call's tiles lie: those of sequence s follow those of the sequences before it, tile after tile; a
@@ -56,8 +58,11 @@ struct Place {
 
 template <int ROWS, int KEYS>
 struct Steps {
+    static constexpr int EXTRA = ROWS == 128 ? 1 : kWaves;
     const CachedArgs &a;
     int begin, end, length, tiles, steps, first; // of this lane's sequence; first: of its steps among those of the 64
+    int total, tile_total, longest;              // of all: steps, tiles, steps of the longest tile
+    bool alone = false;                          // a tile counts as one step
 
     __device__ __forceinline__ Steps(const CachedArgs &args) : a(args) {}
 
@@ -69,15 +74,46 @@ struct Steps {
         length = cached_length(a.c, a.c.lengths[s]);
         tiles = s0 + lane < a.c.count ? (max(end - begin, 0) * a.group + ROWS - 1) / ROWS : 0;
         steps = max((length + KEYS - 1) / KEYS, 1);
-        const int sum = wave_scan(tiles * steps);
-        first = sum - tiles * steps;
+        return scan();
+    }
+    __device__ __forceinline__ int weight() const { return alone ? 1 : steps; }
+    __device__ __forceinline__ int scan()
+    {
+        const int sum = wave_scan(tiles * weight());
+        first = sum - tiles * weight();
         return __builtin_amdgcn_readlane(sum, 63);
     }
     __device__ __forceinline__ int all()
     {
-        int total = 0;
-        for (int s0 = 0; s0 < a.c.count; s0 += 64) total += load(s0);
+        total = tile_total = longest = 0;
+        for (int s0 = 0; s0 < a.c.count; s0 += 64) {
+            total += load(s0);
+            tile_total += __builtin_amdgcn_readlane(wave_scan(tiles), 63);
+            longest = max(longest, __builtin_amdgcn_readfirstlane((int)wave_max_bits(tiles ? (unsigned)steps : 0u)));
+        }
         return total;
+    }
+    // (after all()) Whether wavefronts take whole tiles, each its own, and not eight of them a part together.  In half
+    // microseconds, a tile costs a wavefront 6 and each of its steps 1, a workgroup 9 and an eighth of them.
+    __device__ __forceinline__ bool tiles_alone()
+    {
+        const int rounds = (tile_total + a.parts * kWaves - 1) / (a.parts * kWaves);
+        const float own = (float)rounds * (float)(6 + longest) * (float)a.parts;
+        const float together = 9.0f * (float)max(tile_total, a.parts) + 0.125f * (float)total;
+        alone = __builtin_amdgcn_readfirstlane(own < together ? 1 : 0) != 0;
+        if (alone && a.c.count <= 64) scan();
+        return alone;
+    }
+    // (after all()) Part i of the steps is i * width .. (i + 1) * width - 1.
+    __device__ __forceinline__ int width()
+    {
+        const float tile = (float)total / (float)max(tile_total, 1);         // steps of one
+        const int even = max(divide(total + a.parts - 1, a.by_parts), min(a.least, (int)tile));
+        // where all tiles have as many, parts that begin and end with them, if it takes a step for each wavefront more at most
+        // (us without / with: 8 sequences of 700 tokens, 4 rows, 64 heads over 8, 23 / 17, 16 of 300, 9 rows, 25 / 23)
+        const int fitting = (int)ceilf(tile / fmaxf(floorf(tile / (float)even), 1.0f));
+        const bool fits = tile_total > 1 && longest * tile_total == total && fitting > even && fitting <= even + EXTRA;
+        return __builtin_amdgcn_readfirstlane(fits ? fitting : even);
     }
     __device__ __forceinline__ Place find(int at)        // (after all(); at below it)
     {
@@ -88,7 +124,7 @@ struct Steps {
             const int lane = threadIdx.x & 63;
             int sum = 0;
             if (a.c.count > 64) sum = load(s0);
-            const unsigned long long hit = __ballot(at - before >= first && at - before < first + tiles * steps);
+            const unsigned long long hit = __ballot(at - before >= first && at - before < first + tiles * weight());
             if (hit) {
                 const int l = __ffsll(hit) - 1;
                 p.id = s0 + l;
@@ -97,8 +133,8 @@ struct Steps {
                 p.length = __builtin_amdgcn_readlane(length, l);
                 p.steps = __builtin_amdgcn_readlane(steps, l);
                 const int from = before + __builtin_amdgcn_readlane(first, l);
-                p.tile = (at - from) / p.steps;
-                p.first = from + p.tile * p.steps;
+                p.tile = alone ? at - from : (at - from) / p.steps;
+                p.first = alone ? at : from + p.tile * p.steps;
                 return p;
             }
             before += sum;
@@ -106,12 +142,6 @@ struct Steps {
         return p;
     }
 };
-
-// Part i of the steps is i * width .. (i + 1) * width - 1.
-__device__ __forceinline__ int part_width(const CachedArgs &a, int total)
-{
-    return max(divide(total + a.parts - 1, a.by_parts), a.least);
-}
 
 __device__ __forceinline__ v4f mfma_h(v8h a, v8h b, v4f c)
 {
@@ -249,14 +279,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i16 = lane & 15;
     const int index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
     Steps<ROWS, 2 * kBlock> all(a);
-    const int total = all.all(), width = part_width(a, total);
-    int at = index * width;
-    const int stop = min(at + width, total);
+    const int total = all.all(), width = all.width();
+    const bool alone = all.tiles_alone();
+    const int every = alone ? 1 : kWaves, mine = alone ? 0 : wave;           // of a piece's steps: mine, mine + every, ..
+    int at = alone ? index + a.parts * wave : index * width;
+    const int stop = alone ? all.tile_total : min(at + width, total);
     while (at < stop) {
         const Place p = all.find(at);
         if (p.id < 0) return;
-        const int end = min(stop, p.first + p.steps);
-        const int first = at - p.first, last = end - p.first;                // steps of the tile
+        const int end = alone ? at + a.parts * kWaves : min(stop, p.first + p.steps);
+        const int first = alone ? 0 : at - p.first, last = alone ? p.steps : end - p.first;      // steps of the tile
         const bool whole = first == 0 && last == p.steps;
         const int rows = min(ROWS, p.n * a.group - p.tile * ROWS);
         // rows of this lane: token, position, query
@@ -335,26 +367,26 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
             }
             take(r, x, lv[0], lv[1], [&](int t) { return codes_to_half(st.v[0][t / 4][t % 4], st.v[1][t / 4][t % 4]); });
         };
-        int s = first + wave;
+        int s = first + mine;
         if (s < done) {
             constexpr int N = 2;                         // steps in registers (three or four: no faster)
             Stage<D> st[N];
             int page[N][2], next[2];
 #pragma unroll
-            for (int u = 0; u < N; ++u) pages(page[u], s + u * kWaves);
+            for (int u = 0; u < N; ++u) pages(page[u], s + u * every);
 #pragma unroll
-            for (int u = 0; u < N - 1; ++u) load(st[u], page[u], s + u * kWaves);
+            for (int u = 0; u < N - 1; ++u) load(st[u], page[u], s + u * every);
             for (bool more = true; more;) {
 #pragma unroll
                 for (int u = 0; u < N; ++u) {
-                    pages(next, s + N * kWaves);
-                    load(st[(u + N - 1) % N], page[(u + N - 1) % N], s + (N - 1) * kWaves);
+                    pages(next, s + N * every);
+                    load(st[(u + N - 1) % N], page[(u + N - 1) % N], s + (N - 1) * every);
                     asm volatile("" ::: "memory");                           // (else the loads sink to their use)
                     __builtin_amdgcn_sched_barrier(0);
                     work(st[u], page[u], s);
                     page[u][0] = next[0];
                     page[u][1] = next[1];
-                    s += kWaves;
+                    s += every;
                     if (s >= done) {
                         more = false;
                         break;
@@ -364,7 +396,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         }
         // the unfinished block's tokens, in fp16, with the tile's last step
         const int tail = p.length - full * kBlock;
-        if (last == p.steps && tail > 0 && seen > full * kBlock && wave == (p.steps - 1 - first) % kWaves) {
+        if (last == p.steps && tail > 0 && seen > full * kBlock && (alone || wave == (p.steps - 1 - first) % kWaves)) {
             if (const uint16_t *recent = B::recent(c, p.id, head)) {
                 float x[RB][2][4];
                 v4f acc[RB];
@@ -403,6 +435,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int k = 0; k < RB; ++k) {
             const float l = across_sum(r.l[k]);
+            if (alone) {
+                if (16 * k + i16 < rows) {
+#pragma unroll
+                    for (int t = 0; t < D / 16; ++t)
+                        store_row(a, p.begin, p.tile * ROWS + 16 * k + i16, head, D, 16 * t + 4 * g, r.o[k][t], l);
+                }
+                continue;
+            }
             __syncthreads();
             if (g == 0) {
                 stat[wave][0][i16] = r.m[k];
@@ -480,7 +520,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
     auto key_swizzle = [](int line) { return D == 128 ? line & 15 : (line >> 1) & 7; };
     auto value_swizzle = [](int line) { return KEYS == 128 ? line & 15 : (line >> 1) & 7; };
     Steps<kStageRows, KEYS> all(a);
-    const int total = all.all(), width = part_width(a, total);
+    const int total = all.all(), width = all.width();
     int at = index * width;
     const int stop = min(at + width, total);
     while (at < stop) {
@@ -761,9 +801,9 @@ __global__ __launch_bounds__(64) void join_kernel(CachedArgs a, Divider by_group
     const int all_groups = divide(blockIdx.x, c.by_kv), head = blockIdx.x - all_groups * c.kv_heads;
     const int index = divide(all_groups, by_groups), group = all_groups - index * (int)by_groups.d;
     Steps<ROWS, KEYS> all(a);
-    const int total = all.all(), width = part_width(a, total);
+    const int total = all.all(), width = all.width();
     const int start = index * width, stop = start + width;
-    if (stop >= total) return;
+    if (stop >= total || (ROWS != kStageRows && all.tiles_alone())) return;
     const Place p = all.find(stop);
     if (p.id < 0 || p.first >= stop || p.first < start) return;
     const int rows = p.n * a.group - p.tile * ROWS;

@@ -315,6 +315,39 @@ def test_cached_attention_of_many_sequences():
     s.check_attention(rng.integers(0, lengths + 1).tolist(), 8)
 
 
+@pytest.mark.parametrize("heads,kv,D,count,most,new", [
+    (32, 16, 64, 60, 500, 2), (16, 16, 128, 100, 200, 1), (40, 20, 128, 33, 90, 9), (64, 32, 64, 5, 40, 6), (12, 12, 64, 200, 64, 3)])
+def test_many_short_sequences(heads, kv, D, count, most, new):
+    """More tiles than workgroups, of few steps each; some without tokens or rows, the last pages not there."""
+    rng = np.random.default_rng([26, D, count])
+    lengths = rng.integers(0, most + 1, count)
+    lengths[:3] = most, 0, 16
+    rows = np.minimum(lengths, new)
+    rows[3] = 0
+    s = Story(rng, count, kv, D, 16, most)
+    s.append((lengths - rows).tolist())
+    s.append(rows.tolist())
+    s.check_attention(rows.tolist(), heads)
+
+
+@pytest.mark.parametrize("heads,kv,D", [(8, 2, 64), (4, 2, 128), (24, 1, 128)])
+def test_long_sequences_with_holes(heads, kv, D):
+    """Pages in the middle that are not there, and no slot, where several workgroups share a tile."""
+    rng = np.random.default_rng([27, D])
+    s = Story(rng, 3, kv, D, 32, 2100)
+    s.append([2075, 1300, 1000])
+    s.append([2, 0, 1])
+    parts, q = (2, 0, 1), normal(rng, 3, heads * D)
+    table = s.table.copy()
+    table[0, 5:9], table[0, 40], table[2, 0] = -1, 2**30, -2**31
+    out = host(fq.cache_attention(s.cache, to_dev(q), heads, fq.Sequences(starts_of(parts), i32(s.lengths()), to_dev(table),
+                                                                        i32([s.slots[0], 0, -1]))))
+    for rows, i, left, first in ((slice(0, 2), 0, np.r_[0:160, 288:1280, 1312:2077], 2075 - 160), (slice(2, 3), 2, np.r_[32:992], 960)):
+        k, v = ref.stored(s.k[i], kv)[left], ref.stored(s.v[i], kv)[left]
+        want, off = ref.grouped(q[rows], k, v, heads, kv, first, D ** -0.5)
+        assert_within(out[rows], want, off, f"sequence {i}")
+
+
 @pytest.mark.parametrize("heads,kv,D", [(8, 1, 64), (16, 2, 128)])
 def test_chunks_of_many_sequences(heads, kv, D):
     """More than 64 rows of a sequence on average, of more than 64 sequences, some without rows, some without tokens."""
