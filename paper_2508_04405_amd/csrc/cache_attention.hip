@@ -14,15 +14,16 @@
 // 2^-12 of itself, as much as the output's own rounding, and averages over the keys.
 //
 // Work is cut evenly: all steps of all tiles of a key head lie in a row, and workgroup i of W takes the i-th part of them,
-// whatever sequences it meets there; a tile that several take leaves running maximum, sum and output of each in the
-// workspace and a second launch joins them in order.  Where there are many tiles of few steps, which would leave a workgroup's
-// wavefronts waiting for one another at every tile, each wavefront takes whole tiles of its own instead (`tiles_alone`: 58
-// sequences of up to 394 tokens of 32 key heads 56 -> 26 us, 38 of up to 23 of 8 36 -> 10, 64 of 1000 of 8 63 -> 49).  A step's loads are 2 KiB a block and lane-contiguous, a step ahead, and
-// non-temporal, since no one reads them again soon (48 sequences of up to 8192 tokens, 64 heads over 8: 87 -> 75 us).
+// whatever sequences it meets there; a tile that several take leaves running maximum, sum and output of each in the workspace
+// and a second launch joins them in order.  Where there are many tiles of few steps, which would leave a workgroup's wavefronts
+// waiting for one another at every tile, each wavefront takes whole tiles of its own instead (`tiles_alone`: 58 sequences of up
+// to 394 tokens of 32 key heads 56 -> 26 us, 38 of up to 23 of 8 36 -> 10, 128 of 1000 of 8 63 -> 49).  A step's loads are 2
+// KiB a block and lane-contiguous, a step ahead, and non-temporal, since no one reads them again soon (48 sequences of up to
+// 8192 tokens, 64 heads over 8: 87 -> 75 us).
 //
 // Bound by memory where the cache is long: those 413 MB in 74 us, 5.6 TB/s of the 6.5 that reads alone reach, one sequence of
 // 131072 tokens, 269 MB, in 48; and the joining launch, 3 to 5 us, which would want a wait between workgroups to go.  A short
-// cache takes the trips one after the other: lengths, table, codes, shares (1100 tokens of 32 heads 6.8 + 3.3 us).
+// cache takes the trips one after the other: lengths, table, codes, shares (1100 tokens of 32 heads 7 + 3.5 us).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"
