@@ -51,7 +51,7 @@ struct CachedArgs {
 
 // Where the steps of a call's tiles lie: those of sequence s follow those of the sequences before it, tile after tile; a
 // tile of ROWS rows has as many of KEYS keys as its sequence's length takes (one, if it has none: someone writes its rows).  A lane
-// holds one of 64 sequences, and where they are more than 64, every question goes through all of them again.
+// holds one of 64 sequences; where they are more, they are gone through 64 at a time, by a question from where the last one ended.
 struct Place {
     int id, begin, n, length, tile, steps;
     int first;                                   // step of all at which the tile begins
@@ -63,6 +63,7 @@ struct Steps {
     const CachedArgs &a;
     int begin, end, length, tiles, steps, first; // of this lane's sequence; first: of its steps among those of the 64
     int total, tile_total, longest;              // of all: steps, tiles, steps of the longest tile
+    int from = 0, before = 0;                    // the 64 in which the last question ended; steps of those before them
     bool alone = false;                          // a tile counts as one step
 
     __device__ __forceinline__ Steps(const CachedArgs &args) : a(args) {}
@@ -73,9 +74,13 @@ struct Steps {
         begin = max(a.c.starts[s], 0);
         end = min(a.c.starts[s + 1], a.c.M);
         length = cached_length(a.c, a.c.lengths[s]);
-        tiles = s0 + lane < a.c.count ? (max(end - begin, 0) * a.group + ROWS - 1) / ROWS : 0;
-        steps = max((length + KEYS - 1) / KEYS, 1);
+        size(s0);
         return scan();
+    }
+    __device__ __forceinline__ void size(int s0)
+    {
+        tiles = s0 + (int)(threadIdx.x & 63) < a.c.count ? (max(end - begin, 0) * a.group + ROWS - 1) / ROWS : 0;
+        steps = max((length + KEYS - 1) / KEYS, 1);
     }
     __device__ __forceinline__ int weight() const { return alone ? 1 : steps; }
     __device__ __forceinline__ int scan()
@@ -116,26 +121,29 @@ struct Steps {
         const bool fits = tile_total > 1 && longest * tile_total == total && fitting > even && fitting <= even + EXTRA;
         return __builtin_amdgcn_readfirstlane(fits ? fitting : even);
     }
-    __device__ __forceinline__ Place find(int at)        // (after all(); at below it)
+    __device__ __forceinline__ Place find(int at)        // (after all(); at below it, and rising from one call to the next)
     {
         Place p{};
         p.id = -1;
-        int before = 0;
-        for (int s0 = 0; s0 < a.c.count; s0 += 64) {
-            const int lane = threadIdx.x & 63;
+        for (; from < a.c.count; from += 64) {
             int sum = 0;
-            if (a.c.count > 64) sum = load(s0);
+            if (a.c.count > 64) {
+                sum = load(from);
+            } else {
+                asm volatile("" : "+v"(begin), "+v"(end), "+v"(length));     // (made again, so that they take no registers meanwhile)
+                size(from);
+            }
             const unsigned long long hit = __ballot(at - before >= first && at - before < first + tiles * weight());
             if (hit) {
                 const int l = __ffsll(hit) - 1;
-                p.id = s0 + l;
+                p.id = from + l;
                 p.begin = __builtin_amdgcn_readlane(begin, l);
                 p.n = __builtin_amdgcn_readlane(end, l) - p.begin;
                 p.length = __builtin_amdgcn_readlane(length, l);
                 p.steps = __builtin_amdgcn_readlane(steps, l);
-                const int from = before + __builtin_amdgcn_readlane(first, l);
-                p.tile = alone ? at - from : (at - from) / p.steps;
-                p.first = alone ? at : from + p.tile * p.steps;
+                const int begins = before + __builtin_amdgcn_readlane(first, l);
+                p.tile = alone ? at - begins : (at - begins) / p.steps;
+                p.first = alone ? at : begins + p.tile * p.steps;
                 return p;
             }
             before += sum;
@@ -795,7 +803,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
 template <int D, int ROWS, int KEYS>
 __global__ __launch_bounds__(64) void join_kernel(CachedArgs a, Divider by_groups)
 {
-    constexpr int Q = D / 4, SHARES = ROWS == kStageRows ? 1 : 64 / Q, HIGH = 64 / Q / SHARES, U = 8;    // Q: lanes of a row
+    constexpr int Q = D / 4, SHARES = ROWS == kStageRows ? 1 : 64 / Q, HIGH = 64 / Q / SHARES, U = SHARES == 1 ? 4 : 8;    // Q: lanes of a row
     __shared__ __attribute__((aligned(16))) float red[SHARES][D];
     __shared__ float stat[SHARES][2];
     const CacheArgs &c = a.c;

@@ -316,9 +316,10 @@ def test_cached_attention_of_many_sequences():
 
 
 @pytest.mark.parametrize("heads,kv,D,count,most,new", [
-    (32, 16, 64, 60, 500, 2), (16, 16, 128, 100, 200, 1), (40, 20, 128, 33, 90, 9), (64, 32, 64, 5, 40, 6), (12, 12, 64, 200, 64, 3)])
-def test_many_short_sequences(heads, kv, D, count, most, new):
-    """More tiles than workgroups, of few steps each; some without tokens or rows, the last pages not there."""
+    (32, 16, 64, 60, 500, 2), (16, 16, 128, 100, 200, 1), (40, 20, 128, 33, 90, 9), (64, 32, 64, 5, 40, 6), (12, 12, 64, 200, 64, 3),
+    (4, 1, 64, 70, 900, 1), (16, 8, 64, 300, 20, 1)])
+def test_many_sequences_of_any_length(heads, kv, D, count, most, new):
+    """Many tiles of few steps each, and of more; some without tokens or rows."""
     rng = np.random.default_rng([26, D, count])
     lengths = rng.integers(0, most + 1, count)
     lengths[:3] = most, 0, 16
