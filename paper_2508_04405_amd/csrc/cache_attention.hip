@@ -103,7 +103,7 @@ struct Steps {
     // microseconds, a tile costs a wavefront 6 and each of its steps 1, a workgroup 9 and an eighth of them.
     __device__ __forceinline__ bool tiles_alone()
     {
-        const int rounds = (tile_total + a.parts * kWaves - 1) / (a.parts * kWaves);
+        const int rounds = divide(tile_total + a.parts * kWaves - 1, a.by_parts) / kWaves;
         const float own = (float)rounds * (float)(6 + longest) * (float)a.parts;
         const float together = 9.0f * (float)max(tile_total, a.parts) + 0.125f * (float)total;
         alone = __builtin_amdgcn_readfirstlane(own < together ? 1 : 0) != 0;
@@ -113,11 +113,12 @@ struct Steps {
     // (after all()) Part i of the steps is i * width .. (i + 1) * width - 1.
     __device__ __forceinline__ int width()
     {
-        const float tile = (float)total / (float)max(tile_total, 1);         // steps of one
-        const int even = max(divide(total + a.parts - 1, a.by_parts), min(a.least, (int)tile));
+        // (quotients by the hardware's reciprocal: a step more or less makes a part longer or shorter, the same for everyone)
+        auto over = [](int x, int y) { return (float)x * __builtin_amdgcn_rcpf((float)max(y, 1)); };
+        const int even = max(divide(total + a.parts - 1, a.by_parts), min(a.least, (int)(over(total, tile_total) + 0.01f)));
         // where all tiles have as many, parts that begin and end with them, if it takes a step for each wavefront more at most
         // (us without / with: 8 sequences of 700 tokens, 4 rows, 64 heads over 8, 23 / 17, 16 of 300, 9 rows, 25 / 23)
-        const int fitting = (int)ceilf(tile / fmaxf(floorf(tile / (float)even), 1.0f));
+        const int fitting = (int)(over(longest, max((int)(over(longest, even) + 0.01f), 1)) + 0.99f);
         const bool fits = tile_total > 1 && longest * tile_total == total && fitting > even && fitting <= even + EXTRA;
         return __builtin_amdgcn_readfirstlane(fits ? fitting : even);
     }
