@@ -563,6 +563,37 @@ def test_a_captured_step_follows_lengths_and_pages():
     del kk, vv
 
 
+@pytest.mark.parametrize("heads,kv,new", [(8, 2, 1), (8, 2, 6), (32, 16, 1), (8, 1, 20)])
+def test_a_captured_call_meets_other_lengths(heads, kv, new):
+    """Lengths, pages and slots that change between replays by so much that work is cut in another way."""
+    rng = np.random.default_rng([28, kv, new])
+    D, count = 64, 3
+    s = Story(rng, count, kv, D, 32, 2100)
+    s.append([2080, 1536, 2000])
+    table, slots = to_dev(s.table), to_dev(s.slots)
+    seqs = fq.Sequences(starts_of([new] * count), i32([32] * count), table, slots)
+    q = torch.zeros((count * new, heads * D), dtype=torch.float16, device=DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(fq.load().flexq_cache_attention_workspace_bytes(count * new, count, heads, kv, D), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fq.cache_attention(s.cache, q, heads, seqs, workspace=ws, out=out)
+    for lengths in ([32, 48, 32], [2080, 1536, 2000], [0, 1536, 32], [32, 32, 32], [512, 512, 512], [2080, 32, 48]):
+        qh = normal(rng, count * new, heads * D)
+        q.copy_(to_dev(qh))
+        seqs.lengths.copy_(i32(lengths))
+        ws.fill_(255)
+        out.fill_(NAN)
+        graph.replay()
+        got = host(out)
+        assert np.array_equal(got, host(fq.cache_attention(s.cache, q, heads, seqs)))
+        for i, L in enumerate(lengths):
+            rows = slice(i * new, (i + 1) * new)
+            want, off = ref.grouped(qh[rows], ref.stored(s.k[i], kv)[:L], ref.stored(s.v[i], kv)[:L], heads, kv, L - new, D ** -0.5)
+            assert_within(got[rows], want, off, f"lengths {lengths} sequence {i}")
+
+
 def test_two_graphs_share_a_workspace():
     """Chunks of two sequences' prompts and single tokens, in graphs of one workspace, replayed in turn with eager calls and a
     changed batch between them."""
