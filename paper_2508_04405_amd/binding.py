@@ -627,12 +627,12 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
 
 def _rows(t, rows, width, dev, exact=True):
     """A view of fp16 rows, [rows, width] or wider ones with exact = False, each contiguous, on device `dev` -> their stride."""
-    s = t.shape
+    s, strides = t.shape, t.stride()
     if (t.get_device() != dev or t.dtype != torch.float16 or len(s) != 2 or s[0] != rows or s[1] < width or (exact and s[1] != width)
-            or t.stride(1) != 1):
+            or strides[1] != 1):
         raise FlexQError(f"flexq: expected fp16 rows [{rows}, {width}] on the current device, got {t.dtype} {list(s)} of strides "
                          f"{list(t.stride())} on {t.device}")
-    return t.stride(0) if rows > 1 else (s[1] + 7) // 8 * 8
+    return strides[0] if rows > 1 else (s[1] + 7) // 8 * 8
 
 
 def _head_dim(t, heads):
