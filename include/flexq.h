@@ -503,8 +503,12 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  * FLEXQ_CACHE_BLOCK tokens of a sequence, from a multiple of it on, are a block; a full block lies in its page as int8 codes
  * with an fp16 scale for its keys and one for its values of each head (those of flexq_quant_act with 8 bits, for the
  * 16 * head_dim values together).  The tokens of the unfinished block stay fp16, with the block before it, in a ring that
- * each sequence has for itself (its slot); so every value is rounded once, whichever way its tokens came, and a sequence
- * may be shortened again (drafts that were turned down) as far back as to the beginning of the block before the unfinished one.
+ * each sequence has for itself (its slot); so every value is rounded once, whichever way its tokens came.
+ * A sequence may be shortened again (drafts that were turned down): by a smaller length, and new tokens behind that.  F the
+ * furthest length it has had, to any length from 16 * (F / 16 - 1) on, whose unfinished block the ring still holds; cuts
+ * do not add up: F stays, however short the sequence was meanwhile.  Further back only to a multiple of FLEXQ_CACHE_BLOCK, which
+ * needs nothing from the ring; the sequence begins anew there: F counts from that length on, and lengths that are no multiple
+ * lie behind it.  The same holds for a sequence that begins with pages of another one, where these end.
  *   codes    dev, 16-byte aligned, pages * flexq_cache_page_bytes(...) bytes: pages are copied and moved as they are
  *   recent   dev, 16-byte aligned, slots * flexq_cache_recent_bytes(...) bytes: slots likewise
  * Neither needs to be initialised.  flexq_sequences, beside starts (the batch's rows are the sequences' newest tokens):

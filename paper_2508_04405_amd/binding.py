@@ -682,7 +682,9 @@ def prompt_attention(q, k, v, heads, kv_heads, starts, scale=None, out=None):
 
 class Cache:
     """Pages of 8-bit keys and values and the sequences' recent tokens (a flexq_cache; keeps the tensors alive): `codes` uint8
-    [pages, page_bytes] and `recent` uint8 [slots, recent_bytes], whose rows are copied and moved as they are."""
+    [pages, page_bytes] and `recent` uint8 [slots, recent_bytes], whose rows are copied and moved as they are.  A sequence may be
+    shortened to any length from 16 * (F // 16 - 1) on, F the furthest it has had, and to every multiple of 16, where it begins
+    anew."""
 
     def __init__(self, pages, page, kv_heads, head_dim, slots, device="cuda"):
         lib = load()

@@ -3,8 +3,9 @@
 // Sixteen tokens of a sequence, from a multiple of sixteen on, are a block. A block that is full lies in its page as 8-bit
 // codes, with one scale for its keys and one for its values of a head: the activation quantizer's codes and scales of the
 // 16 D values.  Until then its tokens wait in fp16, in a ring of 32 tokens that every sequence has: so each value is
-// rounded once, whatever way its block filled up, and the ring still holds the block before the unfinished one, to which a
-// sequence may be shortened.
+// rounded once, whatever way its block filled up, and a sequence may be shortened: token t's place is t mod 32, so the ring holds
+// the last two blocks up to the furthest token that was written, whatever was cut since -- a block before those is under
+// them and does not come back when the sequence is cut a second time.
 //
 // A workgroup takes one block of a sequence and head, its codes through LDS so that they go out 16 bytes a thread; the one that
 // has a sequence's first block -- the only one that reads tokens from the ring -- also writes the new tokens of its last two
