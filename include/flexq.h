@@ -512,7 +512,8 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  *   codes    dev, 16-byte aligned, pages * flexq_cache_page_bytes(...) bytes: pages are copied and moved as they are
  *   recent   dev, 16-byte aligned, slots * flexq_cache_recent_bytes(...) bytes: slots likewise
  * Neither needs to be initialised.  flexq_sequences, beside starts (the batch's rows are the sequences' newest tokens):
- *   lengths  dev, int32 [count]: tokens of each sequence, the batch's among them; beyond what its table has room for, that much
+ *   lengths  dev, int32 [count]: tokens of each sequence, the batch's among them.  Beyond what its table has room for, appends
+ *            drop the tokens that it has none for and reads give zero; attention takes the length for that much
  *   table    dev, int32 [count][max_pages]: its pages in order.  What a page outside 0 .. pages - 1 would hold is not there:
  *            appends drop it, attention does not see it, reads give zero.  Entries behind the length are not looked at
  *   slots    dev, int32 [count], its slot, different ones; outside 0 .. slots - 1 likewise.  NULL: sequence i has slot i

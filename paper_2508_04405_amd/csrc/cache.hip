@@ -58,7 +58,8 @@ __global__ __launch_bounds__(2 * D) void append_kernel(AppendArgs a)
     const int tid = threadIdx.x, index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
     const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, index, c.lengths);
     if (r.id < 0 || r.n == 0) return;
-    const int length = cached_length(c, r.length), first = length - r.n;         // (may be negative: those rows are dropped)
+    const int length = cached_length(c, r.length), first = first_token(c, r.length, r.n);
+    if (first >= length) return;                 // (rows before the first token and behind the table's room are dropped)
     const int b0 = max(first, 0) / kBlock, b = b0 + r.piece, full = length / kBlock;
     const bool leads = r.piece == 0;
     if (b >= full && !leads) return;
@@ -162,10 +163,10 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
     const int tid = threadIdx.x, index = divide(blockIdx.x, c.by_kv), head = blockIdx.x - index * c.kv_heads;
     const RowRange r = find_rows(c.starts, c.count, c.M, 1, kBlock, 2, index, c.lengths);
     if (r.id < 0 || r.n == 0) return;
-    const int length = cached_length(c, r.length), first = length - r.n;
-    // (first may be negative: the block of a negative token has none, its rows are zero)
-    const int b = (first >> 4) + r.piece, full = length / kBlock;
-    if (b * kBlock >= length) return;
+    const int length = cached_length(c, r.length), first = first_token(c, r.length, r.n);
+    // (first may be negative and the end beyond the table's room: rows of tokens that there are not are zero)
+    const int b = (first >> 4) + r.piece, full = length / kBlock, end = first + r.n;
+    if (b * kBlock >= end) return;
     uint16_t *ko = a.k + (size_t)head * D, *vo = a.v + (size_t)head * D;
     auto row = [&](int token) { return (size_t)(r.begin + (token - first)); };
     const int token = tid / (D / 8), d = tid % (D / 8) * 8, quad = tid / (D / 2), dv = tid % (D / 2) * 2;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
                 for (int i = 0; i < 4; ++i) vv[i] = value2(lo >> 8 * i & 255u, hi >> 8 * i & 255u, sv);
             }
         }
-    } else if (b >= 0) {
+    } else if (b >= 0 && b * kBlock < length) {
         if (const uint16_t *recent = B::recent(c, r.id, head)) {
             if (keys) kv = *reinterpret_cast<const uint4 *>(recent + B::recent_key(b * kBlock + token, d));
             if (values) {
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
             }
         }
     }
-    auto mine = [&](int t) { return t >= first && t < length; };
+    auto mine = [&](int t) { return t >= first && t < end; };
     if (keys && mine(b * kBlock + token)) *reinterpret_cast<uint4 *>(ko + row(b * kBlock + token) * a.k_stride + d) = kv;
     if (values) {
 #pragma unroll

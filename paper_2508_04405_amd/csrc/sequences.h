@@ -144,9 +144,17 @@ struct CacheBlock {
     }
 };
 
+__device__ __forceinline__ int cached_room(const CacheArgs &c) { return c.max_pages << (c.shift + 4); }
 __device__ __forceinline__ int cached_length(const CacheArgs &c, int length)
 {
-    return min(max(length, 0), c.max_pages << (c.shift + 4));
+    return min(max(length, 0), cached_room(c));
+}
+
+// Where the n rows of a sequence go, tokens first .. first + n - 1 (first may be negative): by its length as it is given, also
+// where that is beyond the table's room, of which first is the most, so that tokens are counted with 32 bits.
+__device__ __forceinline__ int first_token(const CacheArgs &c, int length, int n)
+{
+    return min(max(length, 0) - n, cached_room(c));
 }
 
 }  // namespace

@@ -1,13 +1,16 @@
 """A block's attention at the edges of what its interface allows, against plain forms in 64 bits (attention_reference)."""
 import numpy as np
 import pytest
+import torch
 
 import attention_reference as ref
+import paper_2508_04405_amd as fq
 from cache_ring import Lengths
-from gpu_helpers import say
-from test_gpu_attention import Story
+from gpu_helpers import say, to_dev
+from test_gpu_attention import Story, host, i32, keys, normal, starts_of
 
 pytestmark = pytest.mark.gpu
+DEV = "cuda"
 
 
 @pytest.mark.parametrize("D,page", [(64, 16), (128, 32)])
@@ -32,3 +35,43 @@ def test_cuts_one_after_the_other(D, page):
         lengths.grow(n)
         s.check_read(s.lengths())
         s.check_attention([min(n, 3), 1], heads)
+
+
+@pytest.mark.parametrize("kv,D,page", [(1, 64, 16), (2, 128, 32), (3, 64, 64)])
+def test_appends_drop_what_the_table_has_no_room_for(kv, D, page):
+    rng = np.random.default_rng([31, D, page])
+    room, width = 64, kv * D
+    s = Story(rng, 2, kv, D, page, room)
+    s.append([64, 20])
+
+    def both(parts, lengths):
+        return fq.Sequences(starts_of(parts), i32(lengths), to_dev(s.table), to_dev(s.slots))
+
+    # a sequence that has no room left stays as it is
+    for n, length in ((1, 65), (1, 66), (16, 80), (40, 104), (5, 2**31 - 1), (3, 2**30), (3, 2**30 + 3)):
+        say(f"{n} rows up to {length}")
+        codes, recent = s.cache.codes.clone(), s.cache.recent.clone()
+        rows = to_dev(normal(rng, n, 2 * width))
+        fq.cache_append(s.cache, rows[:, :width], rows[:, width:], both([n, 0], [length, 20]))
+        assert torch.equal(s.cache.codes, codes) and torch.equal(s.cache.recent, recent)
+        got = torch.full((2, n, width), 5.0, dtype=torch.float16, device=DEV)
+        fq.cache_read(s.cache, both([n, 0], [length, 20]), out=(got[0], got[1]))
+        assert not host(got).any()
+    # of rows that reach across the end of the room, the first ones are taken
+    for at, n in ((60, 7), (48, 30), (33, 64), (0, 70), (63, 1), (63, 2)):
+        say(f"{n} rows behind {at}")
+        s.cut(0, 48 if at > 48 else 0)
+        if len(s.k[0]) < at:
+            s.append([at - len(s.k[0]), 0])
+        k, v = keys(rng, n, width), normal(rng, n, width)
+        s.k[0], s.v[0] = (np.concatenate([a, b])[:room] for a, b in ((s.k[0], k), (s.v[0], v)))
+        fq.cache_append(s.cache, to_dev(k), to_dev(v), both([n, 0], [at + n, 20]))
+        s.check_read(s.lengths())
+        s.check_attention([2, 1], 2 * kv)
+        s.cut(0, 63)
+        s.check_read([63, 20])                       # (from the ring)
+        s.append([1, 0])
+        got = fq.cache_read(s.cache, both([room + 3, 20], [room + 3, 20]), rows=room + 23)
+        for x, rows in zip(got, (s.k, s.v)):
+            assert np.array_equal(host(x)[:room], ref.stored_half(rows[0], kv)) and not host(x)[room:room + 3].any()
+            assert np.array_equal(host(x)[room + 3:], ref.stored_half(rows[1], kv))
