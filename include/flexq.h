@@ -489,7 +489,7 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  *   then by position the pairs (h_i, h_(i + rot/2)), with interleaved = 1 (h_2i, h_(2i+1)), i < rot / 2, through the angle
  *   t = positions[m] * freq[i]:  (a cos t - b sin t, b cos t + a sin t);  elements from rot on are h.
  *   positions  dev, int32 [M]        freq  dev, fp32 [rot/2], radians a position        rot  a multiple of 16
- *   out        dev, rows like x, other columns are left as they were; may be x (with the same stride)
+ *   out        dev, rows like x, other columns are left as they were; may be x (with the same stride, where M > 1)
  * fp32 throughout and one rounding; t is taken modulo a turn in 64 bits, so that far positions are as good as near ones.
  *
  * SEQUENCES of a batch lie one behind the other in its rows: `starts` (dev, int32 [count + 1], ascending from 0) says where each

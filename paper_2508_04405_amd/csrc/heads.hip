@@ -124,7 +124,7 @@ flexq_status flexq_rotate_heads(const uint16_t *x, int x_stride, int M, int head
     if (((long)heads + kv_heads) * head_dim > FLEXQ_MAX_K) return FLEXQ_ESHAPE;
     const int width = (heads + kv_heads) * head_dim;
     if (x_stride < width || out_stride < width || x_stride % 8 != 0 || out_stride % 8 != 0) return FLEXQ_ESHAPE;
-    if (x == out && x_stride != out_stride) return FLEXQ_EINVAL;
+    if (x == out && x_stride != out_stride && M > 1) return FLEXQ_EINVAL;       // (one row has no next one)
     if (!aligned16(x) || !aligned16(out) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(positions) || !aligned4(freq))
         return FLEXQ_EALIGN;
     RotateArgs p{};

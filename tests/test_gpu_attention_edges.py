@@ -7,7 +7,7 @@ import attention_reference as ref
 import paper_2508_04405_amd as fq
 from cache_ring import Lengths
 from gpu_helpers import say, to_dev
-from test_gpu_attention import Story, host, i32, keys, normal, starts_of
+from test_gpu_attention import Story, assert_within, host, i32, keys, normal, starts_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -75,3 +75,21 @@ def test_appends_drop_what_the_table_has_no_room_for(kv, D, page):
         for x, rows in zip(got, (s.k, s.v)):
             assert np.array_equal(host(x)[:room], ref.stored_half(rows[0], kv)) and not host(x)[room:room + 3].any()
             assert np.array_equal(host(x)[room + 3:], ref.stored_half(rows[1], kv))
+
+
+@pytest.mark.parametrize("M", [1, 2])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rotation_in_place_into_a_part_of_the_row(M, norm):
+    """x the fused row, out the part of it that is rotated."""
+    rng = np.random.default_rng([32, M])
+    heads, kv, D = 4, 2, 64
+    width = (heads + kv) * D
+    x, positions = normal(rng, M, width + kv * D), np.arange(7, 7 + M, dtype=np.int32)
+    freq = (10000.0 ** (-np.arange(0, D, 2) / D)).astype(np.float32)
+    g = normal(rng, D) if norm else None
+    want, off = ref.rotate(x, heads, kv, D, positions, freq, g, g)
+    gamma = to_dev(g) if norm else None
+    dx = to_dev(x)
+    fq.rotate_heads(dx, heads, kv, D, to_dev(positions), to_dev(freq), gamma, gamma, out=dx[:, :width])
+    assert_within(host(dx)[:, :width], want, off)
+    assert np.array_equal(host(dx)[:, width:], x[:, width:])
