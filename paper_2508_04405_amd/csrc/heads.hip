@@ -78,7 +78,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
         for (int i = 0; i < 16; ++i) ss += v[i] * v[i];
 #pragma unroll
         for (int d = 1; d < LH; d <<= 1) ss += __shfl_xor(ss, d, 64);
-        const float inv = __builtin_amdgcn_rsqf(ss * (1.0f / D) + p.eps);
+        // (the unit takes numbers below the smallest normal one for zero, whose root's inverse times a head of zeros is NaN)
+        const float inv = __builtin_amdgcn_rsqf(fmaxf(ss * (1.0f / D) + p.eps, 0x1p-126f));
         const uint4 ga = *reinterpret_cast<const uint4 *>(gamma + a0), gb = *reinterpret_cast<const uint4 *>(gamma + b0);
         const unsigned g[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
 #pragma unroll

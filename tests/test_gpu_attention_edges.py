@@ -93,3 +93,18 @@ def test_rotation_in_place_into_a_part_of_the_row(M, norm):
     fq.rotate_heads(dx, heads, kv, D, to_dev(positions), to_dev(freq), gamma, gamma, out=dx[:, :width])
     assert_within(host(dx)[:, :width], want, off)
     assert np.array_equal(host(dx)[:, width:], x[:, width:])
+
+
+@pytest.mark.parametrize("eps", [1.4e-45, 1e-39, 1.2e-38])
+def test_norm_of_zeros_with_the_smallest_eps(eps):
+    rng = np.random.default_rng(33)
+    heads, kv, D, M = 3, 1, 64, 5
+    x = normal(rng, M, (heads + kv) * D)
+    x[1] = 0
+    x[3, D:2 * D] = 0
+    x[4] *= np.float16(6e-8)
+    g, positions = normal(rng, D), np.arange(M, dtype=np.int32)
+    freq = (0.9 ** np.arange(D // 2)).astype(np.float32)
+    want, off = ref.rotate(x, heads, kv, D, positions, freq, g, g, eps)
+    got = host(fq.rotate_heads(to_dev(x), heads, kv, D, to_dev(positions), to_dev(freq), to_dev(g), to_dev(g), eps=eps))
+    assert_within(got, want, off)
