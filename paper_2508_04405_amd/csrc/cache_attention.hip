@@ -522,6 +522,8 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
     constexpr int TASKS = BLOCKS * D / 64 / kStageWaves;           // planes of 1 KiB of a wavefront, of keys and of values
     static_assert(TASKS >= 1, "every wavefront has a plane");
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][KSTAGE + VSTAGE];
+    __shared__ unsigned tail_top[kStageWaves];                     // of the unfinished block's values: largest magnitudes (bits),
+    __shared__ int tail_lift;                                      // and by how many powers of two they are larger in LDS
     const CacheArgs &c = a.c;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, i32 = lane & 31;
     // workgroups 8 apart share an XCD and its L2: each XCD has neighbouring parts, which read the same keys at about the same time
@@ -616,17 +618,38 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                 if (recent && t < tail) w = *reinterpret_cast<const v4u *>(recent + B::recent_key(full * kBlock + t, 8 * chunk));
                 *reinterpret_cast<v4u *>(ks + line * LINE + 16 * (chunk ^ key_swizzle(line))) = w;
             }
-            for (int u = threadIdx.x; u < 4 * D; u += 64 * kStageWaves) {
-                const int g = u & 3, channel = u >> 2;
-                uint16_t w[4] = {0, 0, 0, 0};        // (behind the last token anything may lie)
+            // values below 64 larger by a power of two, exactly, which their scale takes back: with a scale of 1 beside the
+            // small ones of full blocks, weights of a stage would be taken off a maximum that no product reaches
+            constexpr int QUADS = 4 * D / (64 * kStageWaves);                // of a channel's four tokens, a thread
+            uint16_t w[QUADS][4];
+            unsigned most = 0u;
+#pragma unroll
+            for (int n = 0; n < QUADS; ++n) {
+                const int u = threadIdx.x + 64 * kStageWaves * n, g = u & 3, channel = u >> 2;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[n][e] = 0; // (behind the last token anything may lie)
                 if (recent) {
                     const uint16_t *from = recent + B::recent_value(full * kBlock + 4 * g, channel);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (4 * g + e < tail) w[e] = from[e];
+                        if (4 * g + e < tail) w[n][e] = from[e];
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = max(most, w[n][e] & 0x7fffu);
+            }
+            most = wave_max_bits(most);
+            if (lane == 0) tail_top[wave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < kStageWaves; ++n) most = max(most, tail_top[n]);
+            const int lift = most == 0u ? 0 : max(7 - __builtin_amdgcn_frexp_expf(h2f((uint16_t)most)), 0);
+            if (threadIdx.x == 0) tail_lift = lift;
+            const float larger = __uint_as_float((unsigned)(127 + lift) << 23);
+#pragma unroll
+            for (int n = 0; n < QUADS; ++n) {
+                const int u = threadIdx.x + 64 * kStageWaves * n, g = u & 3, channel = u >> 2;
                 *reinterpret_cast<v2u *>(vs + channel * VLINE + 16 * ((2 * b + (g & 1)) ^ value_swizzle(channel)) + 8 * (g >> 1)) =
-                    v2u{(unsigned)w[0] | ((unsigned)w[1] << 16), (unsigned)w[2] | ((unsigned)w[3] << 16)};
+                    v2u{pack_h2(h2f(w[n][0]) * larger, h2f(w[n][1]) * larger), pack_h2(h2f(w[n][2]) * larger, h2f(w[n][3]) * larger)};
             }
         };
         v16f o[D / 32];
@@ -688,7 +711,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
                     const bool code = sc != 0u, ring = has_tail && recent && BLOCKS * s + mine == full;
                     // (a scale is not zero, also where the product is below the smallest number: hidden scores are -inf times it)
                     const float k = code ? fmaxf(h2f((uint16_t)(sc & 0xffffu)) * a.scale, 1e-38f) : a.scale;
-                    const float v = code ? __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16))) : ring ? 0.0f : -INFINITY;
+                    const float v = code ? __builtin_amdgcn_logf(h2f((uint16_t)(sc >> 16))) : ring ? -(float)tail_lift : -INFINITY;
                     const float inv = code || ring ? __builtin_amdgcn_exp2f(-v) : 0.0f;
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b) {

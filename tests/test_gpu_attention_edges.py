@@ -108,3 +108,28 @@ def test_norm_of_zeros_with_the_smallest_eps(eps):
     want, off = ref.rotate(x, heads, kv, D, positions, freq, g, g, eps)
     got = host(fq.rotate_heads(to_dev(x), heads, kv, D, to_dev(positions), to_dev(freq), to_dev(g), to_dev(g), eps=eps))
     assert_within(got, want, off)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new", [1, 3, 10])
+@pytest.mark.parametrize("stages", [0, 3])
+def test_an_unfinished_block_of_tiny_values(D, new, stages):
+    """Equal values of 1e-4, full blocks and an unfinished one whose first key every row prefers by so much that the weights of the
+    others, times their scale of 13 * 2^-24, are numbers of few bits.  The mean of equal values is that value."""
+    heads, stage = 8, 128 if D == 64 else 64
+    length, value = stage * stages + stage - 1, 1651 * 2.0**-24          # 127 codes of that scale
+    rng = np.random.default_rng([34, D, new])
+    s = Story(rng, 1, 1, D, 16, length + 1)
+    for weight in (0.4, 12.45, 12.55, 100.45, 3000.5):                   # of the others: in steps of 2^-33 / 2^-24
+        say(f"D={D} new={new} stages={stages} weight={weight}")
+        k = np.zeros((length, D), np.float16)
+        k[length // 16 * 16, 0] = 1.0
+        s.cut(0, 0)
+        s.append([length], lambda M, w: (k, np.full((M, w), value, np.float16)))
+        q = np.zeros((new, heads * D), np.float16)
+        q[:, ::D] = 16.0
+        scale = float(np.log(13 * 512 / weight) / 16.0)
+        out = host(fq.cache_attention(s.cache, to_dev(q), heads, s.seqs([new]), scale=scale))
+        want, off = ref.grouped(q, ref.stored(k, 1), ref.stored(s.v[0], 1), heads, 1, length - new, scale)
+        assert np.abs(want - value).max() < 1e-12
+        assert_within(out, want, off, f"weight {weight}")
