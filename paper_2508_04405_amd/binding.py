@@ -625,11 +625,14 @@ def adapters(a, b, scale, x, order, offsets, y, workspace=None, out=None):
 
 # ---- a block's attention: rotation of the heads, prompts, an 8-bit cache ------------------------
 
+_INT_MAX = 2**31 - 1             # (ctypes takes larger numbers by their low 32 bits)
+
+
 def _rows(t, rows, width, dev, exact=True):
     """A view of fp16 rows, [rows, width] or wider ones with exact = False, each contiguous, on device `dev` -> their stride."""
     s, strides = t.shape, t.stride()
     if (t.get_device() != dev or t.dtype != torch.float16 or len(s) != 2 or s[0] != rows or s[1] < width or (exact and s[1] != width)
-            or strides[1] != 1):
+            or strides[1] != 1 or (rows > 1 and strides[0] > _INT_MAX)):
         raise FlexQError(f"flexq: expected fp16 rows [{rows}, {width}] on the current device, got {t.dtype} {list(s)} of strides "
                          f"{list(t.stride())} on {t.device}")
     return strides[0] if rows > 1 else (s[1] + 7) // 8 * 8
@@ -704,6 +707,8 @@ class Sequences:
 
     def __init__(self, starts, lengths, table, slots=None):
         cur, (n, pages) = _current(starts), _sizes(table, ("sequences", "pages"))
+        if max(n, pages) > _INT_MAX:
+            raise FlexQError(f"flexq: a table of {n} sequences of {pages} pages")
         _here(starts, torch.int32, (n + 1,), cur)
         _here(lengths, torch.int32, (n,), cur)
         _here(table, torch.int32, (n, pages), cur)
