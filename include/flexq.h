@@ -524,7 +524,8 @@ flexq_status flexq_adapters(const uint16_t *a, const uint16_t *b, const float *s
  *            0 .. L - n + i, out as for prompts, p times a value's scale rounded to fp16.  A row that sees nothing gives zero.
  *            Any n: generation, drafts, the next chunk of a prompt.  Append first.
  *   workspace  flexq_cache_attention_workspace_bytes(M, count, heads, kv_heads, head_dim) bytes, 16-byte aligned, any
- *              content; calls that share it must be ordered on one stream
+ *              content; calls that share it must be ordered on one stream.  More sequences of as many rows need less, not
+ *              more: one that is kept for batches of up to M rows, however many sequences they hold, is sized with count = 1
  * Results are the same every time.  Lengths, pages and slots are read on the device, by captured graphs too.
  */
 #define FLEXQ_CACHE_BLOCK 16
