@@ -498,9 +498,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 // keys is half of a result's registers: its scales are the same in all lanes.  As there, the maximum m that is taken off is
 // raised only where a lane's weights of a block add up to more than 2^15.
 //
-// Bound by the vector unit: 128 rows and 64 keys are 16 to 32 matrix instructions of 32 cycles a wavefront, beside about 250
-// vector ones of four (eight for an exponential), and two wavefronts a SIMD leave gaps in both (56 % and 23 % busy with heads
-// of 64). Codes put into LDS between the matrix instructions, not behind them: slower (95 -> 103 us, at 64 keys a stage).
+// Bound by the vector unit and the matrix pipe, one after the other in both wavefronts of a SIMD: a stage is 32 matrix instructions
+// of 32 cycles a wavefront, beside, with heads of 64 (128 keys), about 470 vector ones -- scores weighed, and codes turned and
+// placed, which only 128 rows share -- of four cycles (eight for an exponential): 63 % and 28 % busy there.  With heads of 128
+// (64 keys) 0.80 PFLOP/s (512 new tokens each of three sequences of up to 8192, 64 heads over 8, 284 us), against 0.51.  Codes
+// put into LDS between the matrix instructions, not behind them: slower (95 -> 103 us, at 64 keys a stage).
 constexpr int kStageWaves = 4, kStageRows = 32 * kStageWaves;
 constexpr int stage_keys(int D) { return D == 64 ? 128 : 64; }
 constexpr float kStageShift = 9.0f, kMost = 32768.0f;
@@ -516,7 +518,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
     typedef CacheBlock<D> B;
     constexpr int KEYS = stage_keys(D), BLOCKS = KEYS / kBlock;
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
-    // keys: a line of D channels each; values: a line of 64 keys for each channel, chunk 2 b + half of 16 bytes holding keys
+    // keys: a line of D channels each; values: a line of KEYS keys for each channel, chunk 2 b + half of 16 bytes holding keys
     // 16 b + 4 half + {0 .. 3, 8 .. 11}; chunks XORed by the line, so that sixteen lines' same chunk meets every bank once
     constexpr int LINE = 2 * D, VLINE = 2 * KEYS, KSTAGE = KEYS * LINE, VSTAGE = D * VLINE;
     constexpr int TASKS = BLOCKS * D / 64 / kStageWaves;           // planes of 1 KiB of a wavefront, of keys and of values
@@ -560,7 +562,7 @@ __global__ __launch_bounds__(64 * kStageWaves) __attribute__((amdgpu_waves_per_e
             for (int m = 0; m < D / 16; ++m) q[m] = *reinterpret_cast<const v8h *>(from + 16 * m + 8 * half);
         }
         v4u k_codes[TASKS], v_codes[TASKS];
-        // lane b, b = 0 .. 3: the table's entry and the scales of block b of a stage, and whether the block is there
+        // lane b, b < BLOCKS: the table's entry and the scales of block b of a stage, and whether the block is there
         int pages = -1;
         unsigned scales = 0u;
         bool there = false;
@@ -886,6 +888,8 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 // times, and with heads of 64 twice (us with 32 / 128 a tile: heads of 128, 64 rows, 16 sequences of 1000 tokens of 8 key heads
 // 20.5 / 30, of 4000 45 / 53, 8 of 4000 of 32 96 / 85, 72 rows, 16 of 4000 of 8, 85 / 56; heads of 64, 35 rows, 40 of 2000 of
 // 6, 42.5 / 34.8, 50 rows, 10 of 3000 of 12, 35 / 32; with 16 / 32 a tile 20 rows, 8 of 4000 of 32 key heads, 86 / 51).
+// The host knows the average only, so a batch of unlike sequences has one kind of tile: a chunk of 512 tokens beside 63 single tokens
+// (4000 to 8000 tokens cached, 64 heads over 8) takes 277 us, the two apart 104 + 134; a chunk of 256 beside them 225, apart 62 + 134.
 int tile_rows(int M, int count, int group, int head_dim)
 {
     const long rows = (long)M * group / count;
@@ -894,7 +898,9 @@ int tile_rows(int M, int count, int group, int head_dim)
 
 // Workgroups of a key head: one a CU in all of the streaming kernel, of eight wavefronts, two of the other.  (Streaming, 1 x 8
 // or 2 x 4 wavefronts a CU, us: 8 rows of 8192 tokens of 64 heads over 8 16.6 / 19.2, 16 sequences of 4000 45 / 60, 48 of up to
-// 8192 80 / 80; two tiles of 32 rows each, 8 sequences of 4000 of 32 key heads, 99 / 81.)
+// 8192 80 / 80; two tiles of 32 rows each, 8 sequences of 4000 of 32 key heads, 99 / 81.)  Counts of key heads that leave CUs
+// over lose nothing: 16 sequences of 2000 tokens of 64, 80, 96 and 128 key heads (256, 240, 192 and 256 workgroups) run at 5.9, 5.9,
+// 6.5 and 6.5 TB/s.
 int parts_for(int kv_heads, int rows)
 {
     const int parts = (rows == kStageRows ? 512 : 256) / kv_heads;

@@ -19,7 +19,10 @@
 // with matrix instructions, one block's beside the next one's scores, took 12 % fewer cycles, but at 1.76 GHz, for 1 % of the
 // time; without any load of keys and values, at 1.6 GHz, it would take 3.65 ms.  Operands of S four reads ahead of the
 // instruction that takes them: 4.31 -> 4.2.  4 wavefronts instead of 8: 4.28, but two workgroups a CU, and so better
-// below some thousand tokens (1024 tokens 32 -> 37 us, packed prompts of 300 37 -> 49 with 8).  Short prompts are bound by the rows
+// below some thousand tokens (1024 tokens 32 -> 37 us, packed prompts of 300 37 -> 49 with 8).  Heads of 64 have half the matrix
+// work to an exponential: the vector unit is 78 % busy, the matrix pipe 55 % (16384 tokens of 24 heads over 6 892 us, 0.92 PFLOP/s).
+// Prompts of some thousand tokens wait for the tiles with most stages: with 1024 tokens of 64 heads over 8, 32 us, a CU is busy
+// for 59 % of the launch, with 2048, 91 us, for 79 %.  Short prompts are bound by the rows
 // themselves and by what a workgroup does before its first stage, about 6000 cycles of trips and 2500 of a first stage (100 of 37
 // tokens, 133 MB, 38 us; nine of 3001 in all, heads of 64, 19: the longest one's twelve stages in a row).
 #include "../../include/flexq.h"
