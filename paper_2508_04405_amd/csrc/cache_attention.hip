@@ -21,9 +21,9 @@
 // KiB a block and lane-contiguous, a step ahead, and non-temporal, since no one reads them again soon (48 sequences of up to
 // 8192 tokens, 64 heads over 8: 87 -> 75 us).
 //
-// Bound by memory where the cache is long: those 413 MB in 74 us, 5.6 TB/s of the 6.5 that reads alone reach, one sequence of
-// 131072 tokens, 269 MB, in 48; and the joining launch, 3 to 5 us, which would want a wait between workgroups to go.  A short
-// cache takes the trips one after the other: lengths, table, codes, shares (1100 tokens of 32 heads 7 + 3.5 us).
+// Bound by memory where the cache is long: those 413 MB in 75 us, 5.5 TB/s of the 6.5 that reads alone reach, one sequence of
+// 131072 tokens, 269 MB, in 50; and the joining launch, 4 to 6 us, which would want a wait between workgroups to go.  A short
+// cache takes the trips one after the other: lengths, table, codes, shares (1100 tokens of 32 heads 7.6 + 3.8 us).
 #include "../../include/flexq.h"
 #include "flexq_device.h"
 #include "flexq_kernels.h"

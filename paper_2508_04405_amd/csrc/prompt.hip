@@ -14,7 +14,7 @@
 // maximum of each stage, a quarter of its vector instructions, is not taken.  p is normal down to 2^-23 of the largest;
 // its sum is fp32, unrounded.
 //
-// What bounds it: power.  16384 tokens of 64 heads over 8 take 4.2 ms, 1.05 PFLOP/s (of what the mask leaves; PyTorch's
+// What bounds it: power.  16384 tokens of 64 heads over 8 take 4.25 ms, 1.03 PFLOP/s (of what the mask leaves; PyTorch's
 // fp16 product of 8192^3 reaches 1.14), the matrix pipe busy 53 % of the cycles at 1.9 GHz.  A form that interleaves exponentials
 // with matrix instructions, one block's beside the next one's scores, took 12 % fewer cycles, but at 1.76 GHz, for 1 % of the
 // time; without any load of keys and values, at 1.6 GHz, it would take 3.65 ms.  Operands of S four reads ahead of the
